@@ -261,6 +261,133 @@ uint64_t rglru_set_wait_limit_ns(uint64_t ns);
  */
 int32_t rglru_query_status(void *workspace, void *cuda_stream);
 
+/*
+ * ---- Around the temporal core -------------------------------------------------------------------------------------------
+ * The operators that the residual block of Section 2 needs next to the recurrence: the normalisation in front of it, and
+ * (rglru_linear*, rglru_linear_attention* below) its projections and a second mixer of the same kind.  The conventions at
+ * the top of this file hold: dense row-major device tensors owned by the caller, fp32 per-channel vectors, sums and
+ * statistics in fp32, asynchronous on `cuda_stream`, errors as return codes, capturable.  Every kernel waits for the work before it
+ * on the stream before it reads or writes global memory.
+ */
+
+/*
+ * Normalisation of the rows of x [rows, N] (Section 2.1 puts the one without centring, RMSNorm, in front of every block):
+ *     mu = mean(x) (0 unless center),  r = 1 / sqrt(mean((x - mu)^2) + eps),  y = (x - mu) r weight + bias
+ * A row may be a token, or a head of a token: [B,T,H,d] with N = d normalises every head.
+ *   x, y          [rows,N] io; y must not overlap x
+ *   weight, bias  [N] fp32, or NULL (1 and 0)
+ *   mean, rstd    [rows] fp32, out: mu and r for the backward, each may be NULL
+ * N up to 2^30, any number of rows.  A row with an infinity or a NaN comes out as arithmetic has it and touches no other row.
+ */
+typedef struct {
+    int64_t rows;
+    int32_t N;
+    int32_t io;      /* rglru_dtype_t */
+    int32_t center;  /* non-zero: layer norm; 0: mean square only */
+    float eps;       /* >= 0 */
+} rglru_norm_shape_t;
+
+int32_t rglru_layer_norm(const rglru_norm_shape_t *shape, const void *x, const float *weight, const float *bias, void *y, float *mean,
+                         float *rstd, void *cuda_stream);
+
+/*
+ * Gradients of rglru_layer_norm for an upstream gradient dy [rows,N]: with xh = (x - mu) r and g = dy weight
+ *     dx = r (g - mean(g) [when centred] - xh mean(g xh)),  dweight = sum_rows dy xh,  dbias = sum_rows dy
+ *   mean          [rows] fp32 as the forward left it; read only when shape->center
+ *   rstd          [rows] fp32 as the forward left it
+ *   dx            [rows,N] io, out; must not overlap dy or x
+ *   dweight, dbias [N] fp32, out, overwritten; each may be NULL.  Summed in a fixed order: two runs give the same bits.
+ *   workspace     rglru_layer_norm_workspace_bytes(shape) bytes, 256-byte aligned; may be NULL when dweight and dbias are
+ */
+size_t rglru_layer_norm_workspace_bytes(const rglru_norm_shape_t *shape);
+int32_t rglru_layer_norm_backward(const rglru_norm_shape_t *shape, const void *dy, const void *x, const float *mean, const float *rstd,
+                                  const float *weight, void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes,
+                                  void *cuda_stream);
+
+/*
+ * Projection with its epilogue (the linears of the recurrent block, Section 2.3: two into it, one of them followed by a GeLU, one out
+ * of it that is added to the residual stream):
+ *     z = x weight^T + bias,  y = act(z) + residual
+ *   x         [M,K] io
+ *   weight    [N,K] io, row n holds the weights of output n
+ *   bias      [N] fp32 or NULL
+ *   residual  [M,N] io or NULL; may be y itself (the residual stream updated in place)
+ *   y         [M,N] io, out; must not overlap x or weight, nor residual in part
+ *   preact    [M,N] io, out or NULL: z, for the backward; must not overlap anything else
+ * Sums are fp32; z is rounded only where it is written, y from the unrounded z.  GeLU(v) = v Phi(v), SiLU(v) = v / (1 + exp(-v)).
+ * flags: RGLRU_FLAG_NONE or RGLRU_FLAG_FORCE_GENERIC.
+ */
+typedef enum { RGLRU_ACT_NONE = 0, RGLRU_ACT_GELU = 1, RGLRU_ACT_SILU = 2 } rglru_activation_t;
+typedef struct {
+    int64_t M;       /* rows (tokens), up to 2^31 - 1 */
+    int32_t K, N;    /* inputs and outputs of a row */
+    int32_t io;      /* rglru_dtype_t */
+    int32_t activation;
+    uint32_t flags;
+} rglru_linear_shape_t;
+
+size_t rglru_linear_workspace_bytes(const rglru_linear_shape_t *shape, int32_t op); /* RGLRU_OP_PREFILL: rglru_linear; RGLRU_OP_BACKWARD */
+int32_t rglru_linear(const rglru_linear_shape_t *shape, const void *x, const void *weight, const float *bias, const void *residual, void *y,
+                     void *preact, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Gradients of rglru_linear for an upstream gradient dy [M,N] (that of residual is dy itself):
+ *     dz = dy act'(z),  dx = dz weight,  dweight = dz^T x,  dbias = sum_rows dz
+ *   preact           [M,N] io, z as the forward wrote it; NULL (not read) for RGLRU_ACT_NONE
+ *   dx [M,K] io, dweight [N,K] io, dbias [N] fp32: out, overwritten, each may be NULL
+ * dweight has the type of weight (rounded once from an fp32 sum); the products take dz in the io type.  No output may
+ * overlap an input or another output.  Fixed order of all sums: two runs give the same bits.
+ */
+int32_t rglru_linear_backward(const rglru_linear_shape_t *shape, const void *dy, const void *x, const void *weight, const void *preact, void *dx,
+                              void *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Linear attention with a decay for each head, a mixer with a state of constant size like the RG-LRU, S [dk,dv] per head:
+ *     S_t = d S_{t-1} + k_t v_t^T,   o_t = scale q_t S_t,   d = exp(log_decay[h])
+ * d is a constant of the layer; no gradient is formed for it.  log_decay is usually negative; 0 is plain linear attention, -inf
+ * forgets everything but the token itself, above 0 the state grows.
+ *   q, k          [B,T,H,dk] io        v, o   [B,T,H,dv] io; o must not overlap q, k or v
+ *   log_decay     [H] fp32
+ *   s0            [B,H,dk,dv] fp32, in, or NULL for a zero state
+ *   s_T           [B,H,dk,dv] fp32, out: the state after the last token; may be s0 itself, must not overlap it in part
+ * `strides` NULL: q, k, v, o (and the gradients below) are dense.  Otherwise each has the distance in elements from a token to the next
+ * and from a sequence to the next, with the heads of a token side by side ({0, 0}: dense), so that q, k and v may be parts of one
+ * projection's output, and time-major batches need no copy.  Tokens must not overlap one another.
+ * Prefill and backward: dk and dv up to 256.  The state and all sums are fp32; bf16 calls round products of q and k, and
+ * the state where an output reads it, to bf16 (s_T and ds0 stay as exact as fp32 sums are).
+ */
+typedef struct { int64_t token, batch; } rglru_stride_t;
+typedef struct { rglru_stride_t q, k, v, o, dq, dk, dv; } rglru_linear_attention_strides_t; /* o: also of do */
+typedef struct {
+    int32_t B, T, H; /* T is ignored by the decode step */
+    int32_t dk, dv;
+    int32_t io;      /* rglru_dtype_t */
+    float scale;
+    uint32_t flags;  /* RGLRU_FLAG_NONE or RGLRU_FLAG_FORCE_GENERIC */
+} rglru_linear_attention_shape_t;
+
+size_t rglru_linear_attention_workspace_bytes(const rglru_linear_attention_shape_t *shape, int32_t op);
+int32_t rglru_linear_attention_prefill(const rglru_linear_attention_shape_t *shape, const rglru_linear_attention_strides_t *strides, const void *q,
+                                       const void *k, const void *v, const float *log_decay, const float *s0, void *o, float *s_T,
+                                       void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * One token for each of B sequences: q, k [B,H,dk], v, o [B,H,dv] io, dense; s [B,H,dk,dv] fp32 updated in place.  o must not overlap
+ * q, k or v.  Any dk and dv.
+ */
+int32_t rglru_linear_attention_decode_step(const rglru_linear_attention_shape_t *shape, const void *q, const void *k, const void *v,
+                                           const float *log_decay, float *s, void *o, void *cuda_stream);
+
+/*
+ * Gradients of rglru_linear_attention_prefill for upstream gradients do [B,T,H,dv] on o and (optional) ds_T [B,H,dk,dv] fp32 on s_T:
+ *     G_t = scale q_t do_t^T + d G_{t+1} (ds_T at the end),  dq_t = scale S_t do_t,  dk_t = G_t v_t,  dv_t = k_t G_t,  ds0 = d G_1
+ *   dq, dk, dv    like q, k, v, out; must not overlap an input or one another
+ *   ds0           [B,H,dk,dv] fp32, out, or NULL; must not overlap an input
+ */
+int32_t rglru_linear_attention_backward(const rglru_linear_attention_shape_t *shape, const rglru_linear_attention_strides_t *strides, const void *q,
+                                        const void *k, const void *v, const float *log_decay, const float *s0, const void *dout, const float *ds_T,
+                                        void *dq, void *dk, void *dv, float *ds0, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

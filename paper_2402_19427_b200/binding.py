@@ -21,12 +21,16 @@ HOST_PATH = os.path.join(_PKG, "_host.so")
 OK, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALIGN, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_ALIAS = range(9)
 F32, BF16 = 0, 1
 OP_PREFILL, OP_DECODE, OP_BACKWARD = 0, 1, 2
+ACTIVATIONS = {"none": 0, "gelu": 1, "silu": 2}
 FLAG_NONE, FLAG_FORCE_GENERIC = 0, 1
 FLAG_TEST_CARRY_NEVER_ARRIVES = 0x40000000   # failure-path test hook (see include/rglru.h)
 
 EXPORTED = ["rglru_abi_version", "rglru_status_string", "rglru_workspace_bytes", "rglru_prefill",
             "rglru_decode_step", "rglru_backward", "rglru_host_staging_bytes", "rglru_prefill_host",
-            "rglru_query_status", "rglru_prefill_static_scratch", "rglru_set_wait_limit_ns", "rglru_prefill_ex"]
+            "rglru_query_status", "rglru_prefill_static_scratch", "rglru_set_wait_limit_ns", "rglru_prefill_ex",
+            "rglru_layer_norm", "rglru_layer_norm_workspace_bytes", "rglru_layer_norm_backward", "rglru_linear",
+            "rglru_linear_workspace_bytes", "rglru_linear_backward", "rglru_linear_attention_prefill",
+            "rglru_linear_attention_workspace_bytes", "rglru_linear_attention_decode_step", "rglru_linear_attention_backward"]
 
 
 class Shape(ctypes.Structure):
@@ -38,6 +42,25 @@ class ParamPtrs(ctypes.Structure):
     _fields_ = [("conv_w", ctypes.c_void_p), ("conv_b", ctypes.c_void_p), ("W_a", ctypes.c_void_p),
                 ("b_a", ctypes.c_void_p), ("W_x", ctypes.c_void_p), ("b_x", ctypes.c_void_p),
                 ("lam", ctypes.c_void_p)]
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("N", ctypes.c_int32), ("io", ctypes.c_int32), ("center", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class LinearShape(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int32), ("N", ctypes.c_int32), ("io", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class LinearAttentionShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("dk", ctypes.c_int32), ("dv", ctypes.c_int32),
+                ("io", ctypes.c_int32), ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class LinearAttentionStrides(ctypes.Structure):
+    """(token, batch) distances of q, k, v, o, dq, dk, dv."""
+    _fields_ = [(n, ctypes.c_int64 * 2) for n in ("q", "k", "v", "o", "dq", "dk", "dv")]
 
 
 class RglruError(RuntimeError):
@@ -96,6 +119,22 @@ def load() -> ctypes.CDLL:
         lib.rglru_set_wait_limit_ns.restype = ctypes.c_uint64
         lib.rglru_query_status.argtypes = [vp, vp]
         lib.rglru_query_status.restype = i32
+        np_, lp, ap, tp = (ctypes.POINTER(t) for t in (NormShape, LinearShape, LinearAttentionShape, LinearAttentionStrides))
+        lib.rglru_layer_norm.argtypes = [np_] + [vp] * 7
+        lib.rglru_layer_norm_workspace_bytes.argtypes = [np_]
+        lib.rglru_layer_norm_backward.argtypes = [np_] + [vp] * 9 + [sz, vp]
+        lib.rglru_linear.argtypes = [lp] + [vp] * 7 + [sz, vp]
+        lib.rglru_linear_workspace_bytes.argtypes = [lp, i32]
+        lib.rglru_linear_backward.argtypes = [lp] + [vp] * 8 + [sz, vp]
+        lib.rglru_linear_attention_prefill.argtypes = [ap, tp] + [vp] * 8 + [sz, vp]
+        lib.rglru_linear_attention_workspace_bytes.argtypes = [ap, i32]
+        lib.rglru_linear_attention_decode_step.argtypes = [ap] + [vp] * 7
+        lib.rglru_linear_attention_backward.argtypes = [ap, tp] + [vp] * 12 + [sz, vp]
+        for fn in (lib.rglru_layer_norm, lib.rglru_layer_norm_backward, lib.rglru_linear, lib.rglru_linear_backward,
+                   lib.rglru_linear_attention_prefill, lib.rglru_linear_attention_decode_step, lib.rglru_linear_attention_backward):
+            fn.restype = i32
+        for fn in (lib.rglru_layer_norm_workspace_bytes, lib.rglru_linear_workspace_bytes, lib.rglru_linear_attention_workspace_bytes):
+            fn.restype = sz
         _lib = lib
     return _lib
 
@@ -330,3 +369,57 @@ def set_wait_limit_ns(ns: int) -> int:
 
 def query_status(workspace) -> int:
     return int(load().rglru_query_status(_ptr(workspace), _stream()))
+
+
+# ---- around the temporal core (include/rglru.h has the mathematics and the rules); arguments are checked, outputs allocated and the
+# ---- library called in csrc/host_binding.cpp, on the device and its current stream that the tensors live on
+def layer_norm(x, weight=None, bias=None, eps=1e-5, center=True, stats=False, y=None):
+    """Normalised rows (last dimension) of x: layer norm, or with ``center=False`` the root mean square alone (rglru_layer_norm).
+    weight, bias [N] fp32.  Returns y; with ``stats`` (y, mean, rstd) for :func:`layer_norm_backward` (mean None if not centred)."""
+    return _native().layer_norm(x, weight, bias, eps, center, stats, y)
+
+
+def layer_norm_backward(dy, x, rstd, mean=None, weight=None, param_grads=True, dx=None, workspace=None):
+    """Gradients of :func:`layer_norm` (rglru_layer_norm_backward): dict with x (io dtype) and, with ``param_grads``, weight and bias
+    [N] fp32.  ``mean`` None: the forward did not centre."""
+    return _native().layer_norm_backward(dy, x, rstd, mean, weight, param_grads, dx, workspace)
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation: expected one of {sorted(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+def linear(x, weight, bias=None, activation="none", residual=None, y=None, keep_preact=False, flags=0, workspace=None):
+    """y = act(x weight^T + bias) + residual (rglru_linear): x [..., K], weight [N,K], residual and y [..., N] io dtype, bias [N] fp32;
+    ``y`` may be ``residual``.  Returns y; with ``keep_preact`` (y, what went into the activation) for :func:`linear_backward`."""
+    return _native().linear(x, weight, bias, _activation(activation), residual, y, keep_preact, flags, workspace)
+
+
+def linear_backward(dy, x, weight, preact=None, activation="none", need=("x", "weight", "bias"), flags=0, workspace=None):
+    """Gradients of :func:`linear` (rglru_linear_backward): dict with those of x, weight (io dtype) and bias (fp32) that ``need``
+    names; that of residual is dy."""
+    if not set(need) <= {"x", "weight", "bias"}:
+        raise ValueError(f"need: expected names out of x, weight, bias, got {need!r}")
+    return _native().linear_backward(dy, x, weight, preact, _activation(activation), "x" in need, "weight" in need, "bias" in need, flags, workspace)
+
+
+def linear_attention_prefill(q, k, v, log_decay, s0=None, scale=None, o=None, s_T=None, flags=0, workspace=None):
+    """o, s_T of S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T, o_t = scale q_t S_t (rglru_linear_attention_prefill).
+    q, k [B,T,H,dk], v [B,T,H,dv] io dtype, any distance between tokens and sequences; log_decay [H], s0, s_T [B,H,dk,dv] fp32;
+    scale: dk^-1/2 unless given."""
+    return _native().linear_attention_prefill(q, k, v, log_decay, s0, scale, o, s_T, flags, workspace)
+
+
+def linear_attention_decode_step(q, k, v, log_decay, s, scale=None, o=None):
+    """One token for B sequences (rglru_linear_attention_decode_step): q, k [B,H,dk], v [B,H,dv]; s [B,H,dk,dv] fp32 is updated in
+    place; returns o [B,H,dv]."""
+    return _native().linear_attention_decode_step(q, k, v, log_decay, s, scale, o)
+
+
+def linear_attention_backward(q, k, v, log_decay, do, s0=None, ds_T=None, scale=None, state_grads=False, dq=None, dk=None, dv=None,
+                              flags=0, workspace=None):
+    """Gradients of sum(do*o) [+ sum(ds_T*s_T)] (rglru_linear_attention_backward): dict with q, k, v (io dtype) and with
+    ``state_grads`` s0 (fp32).  dq, dk, dv: buffers for them, strided like q, k, v may be."""
+    return _native().linear_attention_backward(q, k, v, log_decay, do, s0, ds_T, scale, state_grads, dq, dk, dv, flags, workspace)

@@ -12,9 +12,6 @@ using namespace rglru;
 
 namespace {
 
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-inline size_t io_bytes(int io) { return io == RGLRU_BF16 ? 2 : 4; }
-
 int32_t check_shape(const rglru_shape_t *s, bool need_T) {
     if (s == nullptr) return RGLRU_ERR_NULL;
     if (s->B <= 0 || s->D <= 0 || s->H <= 0 || (need_T && s->T <= 0)) return RGLRU_ERR_SHAPE;
@@ -32,12 +29,6 @@ int32_t check_params(const rglru_params_t *p) {
         !aligned(p->b_x, 16) || !aligned(p->lambda, 16) || !aligned(p->conv_b, 16))
         return RGLRU_ERR_ALIGN;
     return RGLRU_OK;
-}
-
-inline bool overlap(const void *a, size_t na, const void *b, size_t nb) {
-    if (!a || !b) return false;
-    uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
-    return pa < pb + nb && pb < pa + na;
 }
 
 bool use_sm100_prefill(const rglru_shape_t *s) {

@@ -51,6 +51,15 @@ cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block, size_t
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
+// Argument checks of the entry points
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline size_t io_bytes(int io) { return io == RGLRU_BF16 ? 2 : 4; }
+inline bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    if (!a || !b) return false;
+    uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+    return pa < pb + nb && pb < pa + na;
+}
+
 inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 inline int ceil_div(size_t a, size_t b) { return (int)((a + b - 1) / b); }
 inline int num_sms() {

@@ -1,0 +1,38 @@
+// Linear attention with a decay for each head: what its kernels share.
+//
+// Forward and backward are the same walk.  With (q, k, v, S) standing for one of four sets of tensors, over tokens in walking order
+//     out_i = sp sum_{j <= i} d^(i-j) (q_i k_j) v_j + si d^(i+first) q_i S_in,   S_out = d^n S_in + su sum_j d^(n-j-first) k_j v_j^T
+//   output   (q, k, v),   S0,             first 1, sp = si = scale, su = 1
+//   dq       (do, v, k),  S0 transposed,  first 1, sp = si = scale, su = 1
+//   dk       (v, do, q),  dS_T transposed, last token first, first 0, sp = su = scale, si = 1
+//   dv       (k, q, do),  dS_T,           last token first, first 0, sp = su = scale, si = 1;  its S_out is dS0
+// The tokens of a chunk go through matrix products, the state goes from chunk to chunk.
+#pragma once
+
+#include "rglru_internal.h"
+
+namespace rglru {
+
+struct MixTensor {
+    void *p;
+    long long token, batch;   // distances in elements
+};
+struct MixRole {
+    MixTensor q, k, v, o;
+    int dk, dv;               // widths of q and k, and of v and o
+    const float *s_in;        // [B,H,dk,dv], transposed [B,H,dv,dk] if turned, or null
+    float *s_out;             // [B,H,dk,dv] or null
+    int turned, reverse, first;
+    float sp, si, su;
+};
+struct MixArgs {
+    MixRole role[3];
+    int roles, B, T, H;
+    const float *log_decay;
+    uint32_t *status;
+};
+
+// decay^n; n = 0 is 1 whatever the decay (log_decay may be minus infinity)
+__device__ __forceinline__ float decay_power(float log_decay, float n) { return n == 0.0f ? 1.0f : expf(log_decay * n); }
+
+}  // namespace rglru

@@ -1,0 +1,236 @@
+// Projection with bias, activation and residual in its epilogue, and its gradients: extern "C" entry points, the kernels for any
+// shape and type on the CUDA cores, and the element-wise part of the backward.
+//
+//   forward   z = x W^T + b,  y = act(z) + residual
+//   backward  dz = dy act'(z),  dx = dz W,  dW = dz^T x,  db = sum_rows dz
+#include <cuda_bf16.h>
+
+#include "rglru_linear.cuh"
+
+namespace rglru {
+namespace {
+
+using namespace ptx;
+
+// C[m][n] = sum_k A(m,k) B(n,k) in fp32 on the CUDA cores, 128 x 128 results a block, 8 x 8 a thread, K in steps of 16 through shared
+// memory.  A(m,k) = a[m a_m + k a_k], B(n,k) = b[n b_n + k b_k]: the forward has K innermost in both, dx in A alone, dW in neither.
+constexpr int GT = 128, GK = 16;
+struct GenericGemm {
+    const void *a, *b;
+    long long a_m, a_k, b_n, b_k, M, N, K;
+    LinearEpilogue e;
+};
+template <typename IO> __device__ __forceinline__ float at(const void *p, long long i) {
+    if constexpr (sizeof(IO) == 4) return ((const float *)p)[i];
+    else return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
+}
+template <typename IO> __device__ __forceinline__ void put(void *p, long long i, float v) {
+    if constexpr (sizeof(IO) == 4) ((float *)p)[i] = v;
+    else ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
+}
+template <typename IO> __global__ void __launch_bounds__(256) generic_linear_kernel(GenericGemm g) {
+    __shared__ float sa[GK][GT + 4], sb[GK][GT + 4];
+    dependency_wait();
+    const long long tiles_n = (g.N + GT - 1) / GT, m0 = blockIdx.x / tiles_n * GT, n0 = blockIdx.x % tiles_n * GT;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    float acc[8][8] = {};
+    for (long long k0 = 0; k0 < g.K; k0 += GK) {
+        // neighbouring threads read along whichever dimension is innermost in memory
+#pragma unroll
+        for (int i = 0; i < GT * GK / 256; ++i) {
+            const int at_ = threadIdx.x + i * 256;
+            const int ka = g.a_k == 1 ? at_ % GK : at_ / GT, ma = g.a_k == 1 ? at_ / GK : at_ % GT;
+            sa[ka][ma] = m0 + ma < g.M && k0 + ka < g.K ? at<IO>(g.a, (m0 + ma) * g.a_m + (k0 + ka) * g.a_k) : 0.0f;
+            const int kb = g.b_k == 1 ? at_ % GK : at_ / GT, nb = g.b_k == 1 ? at_ / GK : at_ % GT;
+            sb[kb][nb] = n0 + nb < g.N && k0 + kb < g.K ? at<IO>(g.b, (n0 + nb) * g.b_n + (k0 + kb) * g.b_k) : 0.0f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < GK; ++k) {
+            float a[8], b[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 va = *(const float4 *)&sa[k][h * 64 + ty * 4], vb = *(const float4 *)&sb[k][h * 64 + tx * 4];
+                a[4 * h] = va.x; a[4 * h + 1] = va.y; a[4 * h + 2] = va.z; a[4 * h + 3] = va.w;
+                b[4 * h] = vb.x; b[4 * h + 1] = vb.y; b[4 * h + 2] = vb.z; b[4 * h + 3] = vb.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        }
+        __syncthreads();
+    }
+    const LinearEpilogue &e = g.e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const long long m = m0 + (i >> 2) * 64 + ty * 4 + (i & 3);
+        if (m >= g.M) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const long long n = n0 + (j >> 2) * 64 + tx * 4 + (j & 3);
+            if (n >= g.N) continue;
+            const long long o = m * g.N + n;
+            const float z = acc[i][j] + (e.bias ? e.bias[n] : 0.0f);
+            if (e.preact) put<IO>(e.preact, o, z);
+            const float y = activate(z, e.activation) + (e.residual ? at<IO>(e.residual, o) : 0.0f);
+            put<IO>(e.y, o, y);
+        }
+    }
+    dependency_trigger();
+}
+
+// dz = dy act'(z) in the io type, and the sums of the unrounded dz over a block's rows.  A thread owns VE columns and walks rows.
+struct DzArgs {
+    long long M;
+    int N, rows;              // rows a block
+    int activation;
+    const void *dy, *preact;
+    void *dz;                 // null: only the sums (no activation: dz is dy)
+    float *part;              // [row blocks][N] or null
+};
+template <typename IO, int VE> __global__ void __launch_bounds__(256) linear_dz_kernel(DzArgs a) {
+    __shared__ float red[8][32 * VE];
+    dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = (blockIdx.x * 32 + lane) * VE;
+    const long long r0 = (long long)blockIdx.y * a.rows, r1 = min(a.M, r0 + a.rows);
+    float s[VE] = {};
+    if (c < a.N) {
+#pragma unroll 4
+        for (long long r = r0 + warp; r < r1; r += 8) {
+            const long long o = r * a.N + c;
+            float g[VE];
+            LinearVec<IO, VE>::load((const IO *)a.dy + o, g);
+            if (a.activation != RGLRU_ACT_NONE) {
+                float z[VE];
+                LinearVec<IO, VE>::load((const IO *)a.preact + o, z);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) g[e] *= activation_slope(z[e], a.activation);
+                if (a.dz) LinearVec<IO, VE>::store((IO *)a.dz + o, g);
+            }
+#pragma unroll
+            for (int e = 0; e < VE; ++e) s[e] += g[e];
+        }
+    }
+    dependency_trigger();
+    if (a.part == nullptr) return;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) red[warp][lane * VE + e] = s[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * VE; i += 256) {
+        const int col = blockIdx.x * 32 * VE + i;
+        if (col >= a.N) break;
+        float t = red[0][i];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) t += red[w][i];
+        a.part[(size_t)blockIdx.y * a.N + col] = t;
+    }
+}
+
+// Rows a block of linear_dz_kernel takes: about eight blocks an SM over the whole call, at least 64 rows (eight a warp)
+int dz_rows(const rglru_linear_shape_t *s) {
+    const long long cols = (s->N + 255) / 256, want = s->M * cols / (148 * 8);
+    return (int)(want < 64 ? 64 : want > 4096 ? 4096 : (want + 7) / 8 * 8);
+}
+int dz_blocks(const rglru_linear_shape_t *s) { return ceil_div((size_t)s->M, dz_rows(s)); }
+
+cudaError_t linear_dz(const rglru_linear_shape_t *s, const DzArgs &args, cudaStream_t st) {
+    DzArgs a = args;
+    a.rows = dz_rows(s);
+    const bool f32 = s->io == RGLRU_F32, vec = s->N % (f32 ? 4 : 8) == 0;
+    const dim3 grid(ceil_div(s->N, 32 * (vec ? (f32 ? 4 : 8) : 1)), dz_blocks(s));
+    if (f32) return vec ? launch_dependent(linear_dz_kernel<float, 4>, grid, dim3(256), 0, st, a) : launch_dependent(linear_dz_kernel<float, 1>, grid, dim3(256), 0, st, a);
+    return vec ? launch_dependent(linear_dz_kernel<__nv_bfloat16, 8>, grid, dim3(256), 0, st, a)
+               : launch_dependent(linear_dz_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, st, a);
+}
+
+cudaError_t generic_gemm(const GenericGemm &g, int io, cudaStream_t st) {
+    const long long blocks = (g.M + GT - 1) / GT * ((g.N + GT - 1) / GT);
+    if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+    return launch_dependent(io == RGLRU_F32 ? generic_linear_kernel<float> : generic_linear_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, g);
+}
+
+int32_t check_linear(const rglru_linear_shape_t *s) {
+    if (s == nullptr) return RGLRU_ERR_NULL;
+    if (s->M <= 0 || s->M > INT32_MAX || s->K <= 0 || s->N <= 0) return RGLRU_ERR_SHAPE;
+    if (s->io != RGLRU_F32 && s->io != RGLRU_BF16) return RGLRU_ERR_UNSUPPORTED;
+    if (s->activation < RGLRU_ACT_NONE || s->activation > RGLRU_ACT_SILU) return RGLRU_ERR_UNSUPPORTED;
+    return RGLRU_OK;
+}
+
+}  // namespace
+}  // namespace rglru
+
+using namespace rglru;
+
+extern "C" {
+
+size_t rglru_linear_workspace_bytes(const rglru_linear_shape_t *s, int32_t op) {
+    if (check_linear(s) != RGLRU_OK || (op != RGLRU_OP_PREFILL && op != RGLRU_OP_BACKWARD)) return 0;
+    size_t bytes = WS_HEADER_BYTES;
+    if (op == RGLRU_OP_BACKWARD) {
+        bytes += up256((size_t)dz_blocks(s) * s->N * sizeof(float));
+        if (s->activation != RGLRU_ACT_NONE) bytes += up256((size_t)s->M * s->N * io_bytes(s->io));
+    }
+    return bytes;
+}
+
+int32_t rglru_linear(const rglru_linear_shape_t *s, const void *x, const void *weight, const float *bias, const void *residual, void *y, void *preact,
+                     void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    const int32_t rc = check_linear(s);
+    if (rc != RGLRU_OK) return rc;
+    if (!x || !weight || !y || !workspace) return RGLRU_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(y, 16) || !aligned(preact, 16) ||
+        !aligned(workspace, 256))
+        return RGLRU_ERR_ALIGN;
+    if (workspace_bytes < rglru_linear_workspace_bytes(s, RGLRU_OP_PREFILL)) return RGLRU_ERR_WORKSPACE;
+    const size_t io = io_bytes(s->io), xb = (size_t)s->M * s->K * io, wb = (size_t)s->N * s->K * io, yb = (size_t)s->M * s->N * io;
+    if (overlap(y, yb, x, xb) || overlap(y, yb, weight, wb) || (residual != y && overlap(y, yb, residual, yb)) || overlap(preact, yb, x, xb) ||
+        overlap(preact, yb, weight, wb) || overlap(preact, yb, residual, yb) || overlap(preact, yb, y, yb))
+        return RGLRU_ERR_ALIAS;
+    GenericGemm g{x, weight, s->K, 1, s->K, 1, s->M, s->N, s->K, {bias, residual, y, preact, s->activation}};
+    return call_status(generic_gemm(g, s->io, (cudaStream_t)cuda_stream));
+}
+
+int32_t rglru_linear_backward(const rglru_linear_shape_t *s, const void *dy, const void *x, const void *weight, const void *preact, void *dx, void *dweight,
+                              float *dbias, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    const int32_t rc = check_linear(s);
+    if (rc != RGLRU_OK) return rc;
+    const bool act = s->activation != RGLRU_ACT_NONE;
+    if (!dy || !workspace || (act && !preact) || (dx && !weight) || (dweight && !x)) return RGLRU_ERR_NULL;
+    if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(weight, 16) || !aligned(preact, 16) || !aligned(dx, 16) || !aligned(dweight, 16) ||
+        !aligned(dbias, 16) || !aligned(workspace, 256))
+        return RGLRU_ERR_ALIGN;
+    if (workspace_bytes < rglru_linear_workspace_bytes(s, RGLRU_OP_BACKWARD)) return RGLRU_ERR_WORKSPACE;
+    const size_t io = io_bytes(s->io), xb = (size_t)s->M * s->K * io, wb = (size_t)s->N * s->K * io, yb = (size_t)s->M * s->N * io, bb = (size_t)s->N * 4;
+    const void *const ins[4] = {dy, x, weight, act ? preact : nullptr};
+    const size_t in_bytes[4] = {yb, xb, wb, yb};
+    void *const outs[3] = {dx, dweight, dbias};
+    const size_t out_bytes[3] = {xb, wb, bb};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 4; ++j)
+            if (overlap(outs[i], out_bytes[i], ins[j], in_bytes[j])) return RGLRU_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlap(outs[i], out_bytes[i], outs[j], out_bytes[j])) return RGLRU_ERR_ALIAS;
+    }
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    char *p = (char *)workspace + WS_HEADER_BYTES;
+    float *part = (float *)p;
+    p += up256((size_t)dz_blocks(s) * s->N * sizeof(float));
+    const void *dz = act ? p : dy;
+    cudaError_t e = cudaSuccess;
+    if (act || dbias) e = linear_dz(s, DzArgs{s->M, s->N, 0, s->activation, dy, preact, act ? p : nullptr, dbias ? part : nullptr}, st);
+    if (e == cudaSuccess && dbias) {
+        ReduceJobs jobs{};
+        add_reduce_job(jobs, part, dz_blocks(s), s->N, dbias, s->N, nullptr, 0, nullptr, 0);
+        e = run_reduce_jobs(jobs, st);
+    }
+    if (e == cudaSuccess && dx)
+        e = generic_gemm(GenericGemm{dz, weight, s->N, 1, 1, s->K, s->M, s->K, s->N, {nullptr, nullptr, dx, nullptr, RGLRU_ACT_NONE}}, s->io, st);
+    if (e == cudaSuccess && dweight)
+        e = generic_gemm(GenericGemm{dz, x, 1, s->N, 1, s->K, s->N, s->K, s->M, {nullptr, nullptr, dweight, nullptr, RGLRU_ACT_NONE}}, s->io, st);
+    return call_status(e);
+}
+
+}  // extern "C"
