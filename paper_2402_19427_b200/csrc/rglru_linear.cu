@@ -73,7 +73,7 @@ template <typename IO> __global__ void __launch_bounds__(256) generic_linear_ker
             const long long o = m * g.N + n;
             const float z = acc[i][j] + (e.bias ? e.bias[n] : 0.0f);
             if (e.preact) put<IO>(e.preact, o, z);
-            const float y = activate(z, e.activation) + (e.residual ? at<IO>(e.residual, o) : 0.0f);
+            const float y = activate<sizeof(IO) == 2>(z, e.activation) + (e.residual ? at<IO>(e.residual, o) : 0.0f);
             put<IO>(e.y, o, y);
         }
     }
@@ -106,7 +106,7 @@ template <typename IO, int VE> __global__ void __launch_bounds__(256) linear_dz_
                 float z[VE];
                 LinearVec<IO, VE>::load((const IO *)a.preact + o, z);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) g[e] *= activation_slope(z[e], a.activation);
+                for (int e = 0; e < VE; ++e) g[e] *= activation_slope<sizeof(IO) == 2>(z[e], a.activation);
                 if (a.dz) LinearVec<IO, VE>::store((IO *)a.dz + o, g);
             }
 #pragma unroll
@@ -151,6 +151,25 @@ cudaError_t generic_gemm(const GenericGemm &g, int io, cudaStream_t st) {
     return launch_dependent(io == RGLRU_F32 ? generic_linear_kernel<float> : generic_linear_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, g);
 }
 
+// The three products of a call; buffers may be null where only sizes matter
+LinearProduct forward_product(const rglru_linear_shape_t *s, const void *x, const void *weight, const LinearEpilogue &e) {
+    return {{x, s->M, s->K, false}, {weight, s->N, s->K, false}, s->M, s->N, s->K, s->io, e};
+}
+LinearProduct dx_product(const rglru_linear_shape_t *s, const void *dz, const void *weight, void *dx) {
+    return {{dz, s->M, s->N, false}, {weight, s->N, s->K, true}, s->M, s->K, s->N, s->io, {nullptr, nullptr, dx, nullptr, RGLRU_ACT_NONE}};
+}
+LinearProduct dw_product(const rglru_linear_shape_t *s, const void *dz, const void *x, void *dweight) {
+    return {{dz, s->M, s->N, true}, {x, s->M, s->K, true}, s->N, s->K, s->M, s->io, {nullptr, nullptr, dweight, nullptr, RGLRU_ACT_NONE}};
+}
+bool on_tensor_cores(const rglru_linear_shape_t *s, const LinearProduct &g) { return !(s->flags & RGLRU_FLAG_FORCE_GENERIC) && sm100_linear_wanted(g); }
+size_t product_bytes(const rglru_linear_shape_t *s, const LinearProduct &g) { return on_tensor_cores(s, g) ? sm100_linear_bytes(g) : 0; }
+cudaError_t run_product(const rglru_linear_shape_t *s, const LinearProduct &g, void *scratch, void *workspace, cudaStream_t st) {
+    if (on_tensor_cores(s, g)) return sm100_linear(g, scratch, (uint32_t *)workspace, st);
+    auto by_row = [](const LinearOperand &o) { return o.turned ? 1ll : o.cols; };
+    auto by_k = [](const LinearOperand &o) { return o.turned ? o.cols : 1ll; };
+    return generic_gemm(GenericGemm{g.a.p, g.b.p, by_row(g.a), by_k(g.a), by_row(g.b), by_k(g.b), g.M, g.N, g.K, g.e}, g.io, st);
+}
+
 int32_t check_linear(const rglru_linear_shape_t *s) {
     if (s == nullptr) return RGLRU_ERR_NULL;
     if (s->M <= 0 || s->M > INT32_MAX || s->K <= 0 || s->N <= 0) return RGLRU_ERR_SHAPE;
@@ -168,12 +187,11 @@ extern "C" {
 
 size_t rglru_linear_workspace_bytes(const rglru_linear_shape_t *s, int32_t op) {
     if (check_linear(s) != RGLRU_OK || (op != RGLRU_OP_PREFILL && op != RGLRU_OP_BACKWARD)) return 0;
-    size_t bytes = WS_HEADER_BYTES;
-    if (op == RGLRU_OP_BACKWARD) {
-        bytes += up256((size_t)dz_blocks(s) * s->N * sizeof(float));
-        if (s->activation != RGLRU_ACT_NONE) bytes += up256((size_t)s->M * s->N * io_bytes(s->io));
-    }
-    return bytes;
+    if (op == RGLRU_OP_PREFILL) return WS_HEADER_BYTES + product_bytes(s, forward_product(s, nullptr, nullptr, {}));
+    size_t bytes = WS_HEADER_BYTES + up256((size_t)dz_blocks(s) * s->N * sizeof(float));
+    if (s->activation != RGLRU_ACT_NONE) bytes += up256((size_t)s->M * s->N * io_bytes(s->io));
+    const size_t dx = product_bytes(s, dx_product(s, nullptr, nullptr, nullptr)), dw = product_bytes(s, dw_product(s, nullptr, nullptr, nullptr));
+    return bytes + (dx > dw ? dx : dw);   // one after the other
 }
 
 int32_t rglru_linear(const rglru_linear_shape_t *s, const void *x, const void *weight, const float *bias, const void *residual, void *y, void *preact,
@@ -189,8 +207,8 @@ int32_t rglru_linear(const rglru_linear_shape_t *s, const void *x, const void *w
     if (overlap(y, yb, x, xb) || overlap(y, yb, weight, wb) || (residual != y && overlap(y, yb, residual, yb)) || overlap(preact, yb, x, xb) ||
         overlap(preact, yb, weight, wb) || overlap(preact, yb, residual, yb) || overlap(preact, yb, y, yb))
         return RGLRU_ERR_ALIAS;
-    GenericGemm g{x, weight, s->K, 1, s->K, 1, s->M, s->N, s->K, {bias, residual, y, preact, s->activation}};
-    return call_status(generic_gemm(g, s->io, (cudaStream_t)cuda_stream));
+    const LinearProduct g = forward_product(s, x, weight, {bias, residual, y, preact, s->activation});
+    return call_status(run_product(s, g, (char *)workspace + WS_HEADER_BYTES, workspace, (cudaStream_t)cuda_stream));
 }
 
 int32_t rglru_linear_backward(const rglru_linear_shape_t *s, const void *dy, const void *x, const void *weight, const void *preact, void *dx, void *dweight,
@@ -219,6 +237,7 @@ int32_t rglru_linear_backward(const rglru_linear_shape_t *s, const void *dy, con
     float *part = (float *)p;
     p += up256((size_t)dz_blocks(s) * s->N * sizeof(float));
     const void *dz = act ? p : dy;
+    char *scratch = p + (act ? up256((size_t)s->M * s->N * io_bytes(s->io)) : 0);
     cudaError_t e = cudaSuccess;
     if (act || dbias) e = linear_dz(s, DzArgs{s->M, s->N, 0, s->activation, dy, preact, act ? p : nullptr, dbias ? part : nullptr}, st);
     if (e == cudaSuccess && dbias) {
@@ -226,10 +245,8 @@ int32_t rglru_linear_backward(const rglru_linear_shape_t *s, const void *dy, con
         add_reduce_job(jobs, part, dz_blocks(s), s->N, dbias, s->N, nullptr, 0, nullptr, 0);
         e = run_reduce_jobs(jobs, st);
     }
-    if (e == cudaSuccess && dx)
-        e = generic_gemm(GenericGemm{dz, weight, s->N, 1, 1, s->K, s->M, s->K, s->N, {nullptr, nullptr, dx, nullptr, RGLRU_ACT_NONE}}, s->io, st);
-    if (e == cudaSuccess && dweight)
-        e = generic_gemm(GenericGemm{dz, x, 1, s->N, 1, s->K, s->N, s->K, s->M, {nullptr, nullptr, dweight, nullptr, RGLRU_ACT_NONE}}, s->io, st);
+    if (e == cudaSuccess && dx) e = run_product(s, dx_product(s, dz, weight, dx), scratch, workspace, st);
+    if (e == cudaSuccess && dweight) e = run_product(s, dw_product(s, dz, x, dweight), scratch, workspace, st);
     return call_status(e);
 }
 

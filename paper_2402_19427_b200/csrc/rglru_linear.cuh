@@ -15,22 +15,67 @@ struct LinearEpilogue {
     int activation;
 };
 
-constexpr float SQRT_HALF = 0.70710678118654752440f, INV_SQRT_2PI = 0.39894228040143267794f;
-// Phi(z); 0 for minus infinity, where z Phi(z) would be NaN, is dealt with by the callers
-__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-z * SQRT_HALF); }
-__device__ __forceinline__ float sigmoid32(float z) { return 1.0f / (1.0f + expf(-z)); }
-// GeLU and SiLU tend to 0 at minus infinity and their slopes to 0 and 1: what remains is 0 * inf, which arithmetic has as NaN
-__device__ __forceinline__ float activate(float z, int kind) {
-    if (kind == RGLRU_ACT_NONE) return z;
-    if (z == -INFINITY) return 0.0f;
-    return z * (kind == RGLRU_ACT_GELU ? normal_cdf(z) : sigmoid32(z));
+// ---- the products on the tensor cores (rglru_sm100_linear.cu)
+// out[m][n] = epilogue(sum_k A(m,k) B(n,k)).  An operand is a matrix in memory [rows][cols]; `turned`: K runs along its rows.
+struct LinearOperand {
+    const void *p;
+    long long rows, cols;
+    bool turned;
+};
+struct LinearProduct {
+    LinearOperand a, b;
+    long long M, N, K;
+    int io;
+    LinearEpilogue e;
+};
+// Whether the tensor cores serve the product better than the CUDA cores, and the scratch that it takes
+bool sm100_linear_wanted(const LinearProduct &g);
+size_t sm100_linear_bytes(const LinearProduct &g);
+cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status, cudaStream_t st);
+
+// Activations and their slopes, to fp32's last places for fp32 io.  What goes to bf16 takes Phi from the rational approximation 7.1.26 of
+// Abramowitz & Stegun (off by less than 7.5e-8) and the hardware's exponential and reciprocal: a third of the instructions, and the
+// element-wise kernels and epilogues are bound by memory or the tensor cores again.  At the infinities GeLU and SiLU are 0 and
+// infinity, their slopes 0 and 1, where their formulas have 0 * inf.
+constexpr float SQRT_HALF = 0.70710678118654752440f, INV_SQRT_2PI = 0.39894228040143267794f, LOG2_E = 1.44269504088896340736f;
+struct Normal { float tail, density; };   // Phi(-|z|) and exp(-z^2 / 2), for |z| held at 30
+__device__ __forceinline__ Normal normal_tail(float z) {
+    const float a = fabsf(z) > 30.0f ? 30.0f : fabsf(z);   // NaN stays
+    const float t = ptx::rcp_approx(fmaf(a, 0.3275911f * SQRT_HALF, 1.0f));
+    float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    p = fmaf(p, t, 0.5f * 1.421413741f); p = fmaf(p, t, 0.5f * -0.284496736f); p = fmaf(p, t, 0.5f * 0.254829592f);
+    const float e = ptx::ex2_approx(a * a * (-0.5f * LOG2_E));
+    return {p * t * e, e};
 }
-__device__ __forceinline__ float activation_slope(float z, int kind) {
+template <bool FAST> __device__ __forceinline__ float sigmoid_of(float z) {
+    if constexpr (FAST) return ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * z));
+    else return 1.0f / (1.0f + expf(-z));
+}
+template <bool FAST> __device__ __forceinline__ float activate(float z, int kind) {
+    if (kind == RGLRU_ACT_NONE) return z;
+    if (kind == RGLRU_ACT_GELU) {
+        if constexpr (FAST) {
+            const float a = fabsf(z) > 30.0f ? 30.0f : fabsf(z);
+            return fmaf(-a, normal_tail(z).tail, z > 0.0f ? z : 0.0f);
+        } else {
+            return z == -INFINITY ? 0.0f : z * (0.5f * erfcf(-z * SQRT_HALF));
+        }
+    }
+    return z < -100.0f ? 0.0f : z * sigmoid_of<FAST>(z);
+}
+template <bool FAST> __device__ __forceinline__ float activation_slope(float z, int kind) {
     if (kind == RGLRU_ACT_NONE) return 1.0f;
-    if (isinf(z)) return z > 0.0f ? 1.0f : 0.0f;
-    if (kind == RGLRU_ACT_GELU) return fmaf(z * INV_SQRT_2PI, expf(-0.5f * z * z), normal_cdf(z));
-    const float s = sigmoid32(z);
-    return s * fmaf(z, 1.0f - s, 1.0f);
+    if (kind == RGLRU_ACT_GELU) {
+        const float zc = z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z;
+        if constexpr (FAST) {
+            const Normal n = normal_tail(zc);
+            return fmaf(zc * INV_SQRT_2PI, n.density, zc > 0.0f ? 1.0f - n.tail : n.tail);
+        } else {
+            return fmaf(zc * INV_SQRT_2PI, expf(-0.5f * zc * zc), 0.5f * erfcf(-zc * SQRT_HALF));
+        }
+    }
+    const float zc = z > 100.0f ? 100.0f : z < -100.0f ? -100.0f : z, s = sigmoid_of<FAST>(zc);
+    return s * fmaf(zc, 1.0f - s, 1.0f);
 }
 
 template <typename IO, int VE> struct LinearVec {
