@@ -155,6 +155,8 @@ bool encode_bf16_map_3d(CUtensorMap *tm, const void *ptr, uint64_t d0, uint64_t 
 // The general form for any 16-bit element type: dims (innermost first), byte strides of dims 1 and 2, box extents.
 bool encode_map16_3d(CUtensorMap *tm, const void *ptr, const uint64_t dims[3], const uint64_t strides_bytes[2], const uint32_t box[3],
                      bool swizzle128);
+// The same with four dimensions
+bool encode_map16_4d(CUtensorMap *tm, const void *ptr, const uint64_t dims[4], const uint64_t strides_bytes[3], const uint32_t box[4], bool swizzle128);
 // ---- sm_100a backward (bf16 io, D_h a multiple of 32 up to 256, T a multiple of 8): tensor-core GEMMs around element-wise scan kernels
 bool sm100_backward_supported(int B, int T, int D, int H, int io);
 size_t sm100_backward_workspace_bytes(int B, int T, int D, int H);

@@ -231,6 +231,22 @@ bool place(const void *p, const rglru_stride_t &st, const rglru_linear_attention
     return by_token || by_batch;
 }
 const rglru_linear_attention_strides_t DENSE{};
+size_t state_bytes(const rglru_linear_attention_shape_t *s) { return (size_t)s->B * s->H * s->dk * s->dv * sizeof(float); }
+bool may_use_tensor_cores(const rglru_linear_attention_shape_t *s) {
+    return !(s->flags & RGLRU_FLAG_FORCE_GENERIC) && s->io == RGLRU_BF16 && s->dk <= 128 && s->dv <= 128 && s->dk % 8 == 0 && s->dv % 8 == 0;
+}
+cudaError_t run_mix(const rglru_linear_attention_shape_t *s, MixArgs &a, void *workspace, cudaStream_t st) {
+    if (!may_use_tensor_cores(s) || !sm100_mix_supported(a, s->io)) return generic_mix(a, s->io, st);
+    char *scratch = (char *)workspace + WS_HEADER_BYTES;
+    const size_t sums = sm100_mix_bytes(a.roles, s->B, s->T, s->H);
+    if (sums && a.role[0].s_in && a.role[0].s_in == a.role[0].s_out) {   // blocks that share a sequence all read its s0
+        float *copy = (float *)(scratch + up256(sums));
+        const cudaError_t e = cudaMemcpyAsync(copy, a.role[0].s_in, state_bytes(s), cudaMemcpyDeviceToDevice, st);
+        if (e != cudaSuccess) return e;
+        a.role[0].s_in = copy;
+    }
+    return sm100_mix(a, scratch, st);
+}
 
 }  // namespace
 }  // namespace rglru
@@ -242,7 +258,12 @@ extern "C" {
 size_t rglru_linear_attention_workspace_bytes(const rglru_linear_attention_shape_t *s, int32_t op) {
     if (op != RGLRU_OP_PREFILL && op != RGLRU_OP_BACKWARD) return 0;
     if (check_mix(s, true) != RGLRU_OK) return 0;
-    return WS_HEADER_BYTES;
+    // the copy of s0 is for a call that overwrites it (s_T == s0) while blocks read it
+    const int roles = op == RGLRU_OP_PREFILL ? 1 : 3;
+    size_t bytes = WS_HEADER_BYTES;
+    const size_t sums = may_use_tensor_cores(s) ? sm100_mix_bytes(roles, s->B, s->T, s->H) : 0;
+    if (sums) bytes += up256(sums) + (roles == 1 ? up256(state_bytes(s)) : 0);
+    return bytes;
 }
 
 int32_t rglru_linear_attention_prefill(const rglru_linear_attention_shape_t *s, const rglru_linear_attention_strides_t *strides, const void *q, const void *k,
@@ -267,7 +288,7 @@ int32_t rglru_linear_attention_prefill(const rglru_linear_attention_shape_t *s, 
         return RGLRU_ERR_ALIAS;
     a.roles = 1; a.B = s->B; a.T = s->T; a.H = s->H; a.log_decay = log_decay; a.status = (uint32_t *)workspace;
     r.dk = s->dk; r.dv = s->dv; r.s_in = s0; r.s_out = s_T; r.first = 1; r.sp = r.si = s->scale; r.su = 1.0f;
-    return call_status(generic_mix(a, s->io, (cudaStream_t)cuda_stream));
+    return call_status(run_mix(s, a, workspace, (cudaStream_t)cuda_stream));
 }
 
 int32_t rglru_linear_attention_decode_step(const rglru_linear_attention_shape_t *s, const void *q, const void *k, const void *v, const float *log_decay,
@@ -329,7 +350,7 @@ int32_t rglru_linear_attention_backward(const rglru_linear_attention_shape_t *s,
     a.role[0] = MixRole{t[3], t[2], t[1], t[4], s->dv, s->dk, s0, nullptr, 1, 0, 1, s->scale, s->scale, 1.0f};
     a.role[1] = MixRole{t[2], t[3], t[0], t[5], s->dv, s->dk, ds_T, nullptr, 1, 1, 0, s->scale, 1.0f, s->scale};
     a.role[2] = MixRole{t[1], t[0], t[3], t[6], s->dk, s->dv, ds_T, ds0, 0, 1, 0, s->scale, 1.0f, s->scale};
-    return call_status(generic_mix(a, s->io, (cudaStream_t)cuda_stream));
+    return call_status(run_mix(s, a, workspace, (cudaStream_t)cuda_stream));
 }
 
 }  // extern "C"

@@ -208,6 +208,11 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const CUtensorMap
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst_smem), "l"(tm), "r"(c0), "r"(t), "r"(b), "r"(bar) : "memory");
 }
+// the same with four coordinates
+__device__ __forceinline__ void tma_load_4d(uint32_t dst_smem, const CUtensorMap *tm, int c0, int c1, int c2, int c3, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst_smem), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
 // the descriptor of a tiled copy on its way to the descriptor cache (its fetch is the longest part of a first copy)
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(tm) : "memory"); }
 // one tiled TMA store; rows at or beyond T are clipped by the tensor bounds
@@ -257,7 +262,7 @@ __device__ __forceinline__ float f16_bits_to_f32(uint16_t h) { float r; asm("cvt
 // The same, kept in program order with respect to the other volatile statements around it: a conversion placed before a
 // barrier arrive proves that the load which produced its operand has completed by then.
 __device__ __forceinline__ float f16_bits_to_f32_ordered(uint16_t h) { float r; asm volatile("cvt.f32.f16 %0, %1;" : "=f"(r) : "h"(h)); return r; }
-// the same descriptor with bf16 A and B
+// the same descriptor with bf16 A and B (K-major; bits 15 and 16: A, B MN-major)
 __host__ __device__ constexpr uint32_t make_idesc(int M, int N) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
