@@ -9,9 +9,9 @@
 // has to be as exact as fp32 sums are, so the decayed k enters U as three bf16 values that add up to it; P and S enter once.
 //
 // Bound by memory: a chunk of 128 x 128 moves 128 KB, 3.0 us of an SM's share of the measured copy rate; the products take 1.7 us.  One block
-// an SM: 224 KB of q, k, v, the planes of k and S.  Each tile is requested again as soon as its last reader is done: q after the
+// an SM: 224 KB of q, k (twice), v, S, a ring for the planes of k, and outputs on their way.  Each tile is requested again as soon as its last reader is done: q after the
 // far product, k after the scores and planes, v at the chunk's end.  Warps: four turn P into the operand of the near product (in tensor memory,
-// over the scores) and write the outputs, eight make the planes and keep the state, one copies, one issues.
+// over the scores), look through v and write the outputs, eight make the planes and keep the state, one copies, one issues.
 //
 // Blocks share the chunks of all (role, sequence, head) evenly, in order; a block that begins inside a sequence takes the state before it
 // from the sums that a first launch (planes and state product only) leaves for the stretches in front of it.
@@ -29,16 +29,22 @@ using namespace ptx;
 constexpr int CH = 128;                          // tokens a chunk
 constexpr int P_WARPS = 4, S_WARPS = 8, THREADS = (P_WARPS + S_WARPS + 2) * 32;
 constexpr uint32_t BLOCK = 128 * 128;            // 128 rows of 64 bf16
-constexpr uint32_t SM_Q = 0, SM_K = 2 * BLOCK, SM_V = 4 * BLOCK, SM_PLANES = 6 * BLOCK, SM_S = 12 * BLOCK, SM_BAR = 14 * BLOCK;
-enum { QF, KF, VF, QE, KE, VE, SC, PR, PL, VK, DSF, SR, OF, OE, TB, NBAR };
-constexpr uint32_t SM_TMEM = SM_BAR + NBAR * 8, SM_TAB = SM_TMEM + 16, SM_BAD = SM_TAB + (32 + CH) * 4,
-                   SM_TOTAL = SM_BAD + 3 * 132, SM_ALLOC = SM_TOTAL + 1024;
+constexpr int PIECES = 4, SLOTS = 2;             // the planes of k: 32 tokens at a time through two slots
+constexpr uint32_t PLANE = 2 * 32 * 128, SLOT = 3 * PLANE;   // 32 tokens of 2 x 64 values
+constexpr uint32_t TILE = 2 * BLOCK;
+constexpr uint32_t SM_Q = 0, SM_K = TILE, SM_V = SM_K + 2 * TILE, SM_S = SM_V + 2 * TILE, SM_PLANES = SM_S + TILE, SM_BAR = SM_PLANES + SLOT;
+enum { QF, QE, SC, PR, DSF, SR, OF, OE, KF, KE = KF + 2, VF = KE + 2, VK = VF + 2, VE = VK + 2, PLF = VE + 2, PLE = PLF + SLOTS, NBAR = PLE + SLOTS };   // two of each for the two tiles of k and v
+constexpr uint32_t SM_TMEM = SM_BAR + NBAR * 8, SM_BAD = SM_TMEM + 16,
+                   SM_TOTAL = SM_BAD + 8 * 132, SM_ALLOC = SM_TOTAL + 1024;
+// The second slot lies in S's place, which is free from the far product to the next S
+__host__ __device__ constexpr uint32_t slot_at(int slot) { return slot == 0 ? SM_PLANES : SM_S; }
+static_assert(SLOT <= TILE, "a slot in S's place");
 static_assert(SM_ALLOC <= 232448, "shared memory of a block");
 constexpr uint32_t TM_P = 0, TM_Y = 128, TM_X = 256, TM_U = 384;   // tensor-memory columns
 constexpr int WALKERS = 148;                     // the plan, and with it the workspace, does not depend on the device
 
 struct WalkArgs {
-    alignas(64) CUtensorMap tm[3][3];            // q, k, v of each role: [B][T][H][width]
+    alignas(64) CUtensorMap tm[3][4];            // q, k, v and the outputs of each role: [B][T][H][width]
     MixArgs m;
     int units, chunks;                           // (role, sequence, head), chunks of each
     int walkers;
@@ -48,20 +54,33 @@ struct WalkArgs {
 // chunks [first, last) of the walk that block w takes, counted over all units
 __device__ __forceinline__ long long share(const WalkArgs &p, int w) { return (long long)p.units * p.chunks * w / p.walkers; }
 
+// One chunk of the walk; next() goes on to the one behind it
 struct Step {
     int role, b, h, chunk, n, t0;                // t0: the tile's first token in memory (negative where a reversed walk ends)
+    bool fresh;                                  // another (role, sequence, head) than the step before
+    __device__ __forceinline__ void tokens(const WalkArgs &p) {
+        n = min(CH, p.m.T - chunk * CH);
+        t0 = p.m.role[role].reverse ? p.m.T - (chunk + 1) * CH : chunk * CH;
+    }
+    __device__ __forceinline__ Step(const WalkArgs &p, long long g) {
+        const int unit = (int)(g / p.chunks), bh = p.m.B * p.m.H;
+        chunk = (int)(g % p.chunks);
+        role = unit / bh;
+        b = unit % bh / p.m.H;
+        h = unit % p.m.H;
+        fresh = true;
+        if (role < p.m.roles) tokens(p);         // not behind the last chunk of the call
+    }
+    __device__ __forceinline__ void next(const WalkArgs &p) {
+        fresh = ++chunk == p.chunks;
+        if (fresh) {
+            chunk = 0;
+            if (++h == p.m.H) { h = 0; if (++b == p.m.B) { b = 0; ++role; } }
+            if (role == p.m.roles) return;
+        }
+        tokens(p);
+    }
 };
-__device__ __forceinline__ Step step_at(const WalkArgs &p, long long g) {
-    Step s;
-    const int unit = (int)(g / p.chunks), bh = p.m.B * p.m.H;
-    s.chunk = (int)(g % p.chunks);
-    s.role = unit / bh;
-    s.b = unit % bh / p.m.H;
-    s.h = unit % p.m.H;
-    s.n = min(CH, p.m.T - s.chunk * CH);
-    s.t0 = p.m.role[s.role].reverse ? p.m.T - (s.chunk + 1) * CH : s.chunk * CH;
-    return s;
-}
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
@@ -70,7 +89,8 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ bool has_no_number(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+// Bits 15 and 31 of the result: whether the two bf16 of w are infinite or NaN (all bits of the exponent set)
+__device__ __forceinline__ uint32_t no_numbers(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
 
 // The values of a 16-byte piece of v that are no numbers become 0 in shared memory: a product would carry them into rows of tokens
 // before theirs, as 0 * NaN.  Byte c of `bad` holds the first token (in walking order) from which on column c is NaN, 255: none.
@@ -102,18 +122,19 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
     auto BAR = [&](int i) { return base + SM_BAR + 8u * i; };
     uint32_t *tmem_base_s = (uint32_t *)(smem + SM_TMEM);
     volatile int *abort_flag = (volatile int *)(tmem_base_s + 1);
-    float *tab = (float *)(smem + SM_TAB);
-    uint32_t *bad_base = (uint32_t *)(smem + SM_BAD);   // [3][33] words, by the step: a byte for each column, and whether there is any
+    uint32_t *bad_base = (uint32_t *)(smem + SM_BAD);   // [8][33] words, by the step: a byte for each column, and whether there is any
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned long long spin = p.spin_ns;
 
     if (tid == 0) {
-        const int count[NBAR] = {1, 1, 1, 1, STATE_ONLY ? S_WARPS : S_WARPS + 1, 1, 1, P_WARPS, S_WARPS, S_WARPS, 1, S_WARPS, 1, P_WARPS, P_WARPS};
-        for (int i = 0; i < NBAR; ++i) mbar_init(BAR(i), count[i]);
+        for (int i = 0; i < NBAR; ++i) {
+            const bool by_p = i == PR || i == OE || i == VK || i == VK + 1 || (!STATE_ONLY && (i == VE || i == VE + 1)), to_k = i == KE || i == KE + 1, by_s = i == SR || to_k || (i >= PLF && i < PLE);
+            mbar_init(BAR(i), by_p ? P_WARPS : by_s ? S_WARPS + (to_k && !STATE_ONLY) : 1);
+        }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (tid < 3 * 33) bad_base[tid] = tid % 33 == 32 ? 0u : 0xFFFFFFFFu;
+    if (tid < 8 * 33) bad_base[tid] = tid % 33 == 32 ? 0u : 0xFFFFFFFFu;
     if (warp == P_WARPS + S_WARPS + 1) { tmem_alloc(smem_u32(tmem_base_s), 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
@@ -131,202 +152,281 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
     const int steps = (int)(last - first);
 
     if (warp == P_WARPS + S_WARPS) {
-        // ---- copies
+        // ---- copies: k and v one chunk ahead of q
         if (lane == 0) {
-            for (int s = 0; s < steps && ok; ++s) {
-                const Step st = step_at(p, first + s);
-                const MixRole &r = p.m.role[st.role];
-                const int kb = r.dk > 64 ? 2 : 1, vb = r.dv > 64 ? 2 : 1;
-                const uint32_t before = (s & 1) ^ 1;
-                if (!STATE_ONLY) {
-                    ok = mbar_wait(BAR(QE), before, spin, abort_flag);
-                    if (!ok) break;
-                    mbar_expect_tx(BAR(QF), kb * BLOCK);
-                    for (int j = 0; j < kb; ++j) tma_load_4d(base + SM_Q + j * BLOCK, &p.tm[st.role][0], j * 64, st.h, st.t0, st.b, BAR(QF));
-                }
-                ok = mbar_wait(BAR(KE), before, spin, abort_flag);
-                if (!ok) break;
-                mbar_expect_tx(BAR(KF), kb * BLOCK);
-                for (int j = 0; j < kb; ++j) tma_load_4d(base + SM_K + j * BLOCK, &p.tm[st.role][1], j * 64, st.h, st.t0, st.b, BAR(KF));
-                ok = mbar_wait(BAR(VE), before, spin, abort_flag);
-                if (!ok) break;
-                mbar_expect_tx(BAR(VF), vb * BLOCK);
-                for (int j = 0; j < vb; ++j) tma_load_4d(base + SM_V + j * BLOCK, &p.tm[st.role][2], j * 64, st.h, st.t0, st.b, BAR(VF));
+            auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
+            auto tile = [&](int which, const Step &st, int width, uint32_t to, int bar) {
+                const int blocks = width > 64 ? 2 : 1;
+                mbar_expect_tx(BAR(bar), blocks * BLOCK);
+                for (int j = 0; j < blocks; ++j) tma_load_4d(base + to + j * BLOCK, &p.tm[st.role][which], j * 64, st.h, st.t0, st.b, BAR(bar));
+            };
+            Step st(p, first), ahead = st;
+            auto load_kv = [&](int s) {
+                const MixRole &r = p.m.role[ahead.role];
+                const int k = s & 1;
+                const uint32_t before = (s >> 1 & 1) ^ 1;
+                if (!wait(KE + k, before)) return;
+                tile(1, ahead, r.dk, SM_K + k * TILE, KF + k);
+                if (!wait(VE + k, before)) return;
+                tile(2, ahead, r.dv, SM_V + k * TILE, VF + k);
+                ahead.next(p);
+            };
+            if (steps > 0) load_kv(0);
+            for (int s = 0; s < steps && ok; ++s, st.next(p)) {
+                if (!STATE_ONLY && wait(QE, (s & 1) ^ 1)) tile(0, st, p.m.role[st.role].dk, SM_Q, QF);
+                if (ok && s + 1 < steps) load_kv(s + 1);
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp == P_WARPS + S_WARPS + 1) {
         // ---- products
+        // Waits never suspend the thread: what it waits for is tens of cycles away, waking up takes hundreds.
         if (lane == 0) {
-            for (int s = 0; s < steps && ok; ++s) {
-                const Step st = step_at(p, first + s);
-                const MixRole &r = p.m.role[st.role];
-                const int ks = r.dk > 64 ? 8 : 4;
-                const uint32_t ph = s & 1, nv = r.dv > 64 ? 128 : 64;
-                const uint32_t id_p = make_idesc(128, 128), id_b = make_idesc(128, nv) | (1u << 16), id_ab = id_b | (1u << 15);
-                auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait(BAR(bar), parity, spin, abort_flag); };
-                if (!STATE_ONLY) {
-                    wait(QF, ph); wait(KF, ph);
-                    if (!ok) break;
-                    tc_fence_after();
-                    for (int k = 0; k < ks; ++k) {
-                        const uint32_t off = (k >> 2) * BLOCK + (k & 3) * 32;
-                        mma_ss(tmem + TM_P, make_desc_sw128(base + SM_Q + off), make_desc_sw128(base + SM_K + off), id_p, k != 0);
-                    }
-                    tc_commit(BAR(SC));
-                    tc_commit(BAR(KE));
-                    wait(SR, ph); wait(OE, ph ^ 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    for (int k = 0; k < ks; ++k)   // S as it lies: a row of 64 columns of v, 128 rows a block
-                        mma_ss(tmem + TM_X, make_desc_sw128(base + SM_Q + (k >> 2) * BLOCK + (k & 3) * 32), make_desc_sw128_mn(base + SM_S + k * 2048, BLOCK), id_b, k != 0);
-                    tc_commit(BAR(QE));
-                } else {
-                    wait(SR, ph);
-                    if (!ok) break;
-                }
-                wait(PL, ph); wait(VK, ph);
-                if (!ok) break;
+            auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); };
+            // descriptors: 16 bytes are one unit of their address field
+            const uint64_t q_k = make_desc_sw128(base + SM_Q), k_k = make_desc_sw128(base + SM_K), v_mn = make_desc_sw128_mn(base + SM_V, BLOCK),
+                           s_mn = make_desc_sw128_mn(base + SM_S, BLOCK), pl_mn = make_desc_sw128_mn(base, PLANE / 2);   // a piece's two blocks of 64 values of k
+            auto scores = [&](int s, const MixRole &r) {
+                wait(QF, s & 1); wait(KF + (s & 1), s >> 1 & 1);
+                if (!ok) return;
                 tc_fence_after();
-                for (int pl = 2; pl >= 0; --pl)   // the smallest first
-                    for (int k = 0; k < 8; ++k)
-                        mma_ss(tmem + TM_U, make_desc_sw128_mn(base + SM_PLANES + pl * 2 * BLOCK + k * 2048, BLOCK), make_desc_sw128_mn(base + SM_V + k * 2048, BLOCK), id_ab,
-                               (pl != 2) | (k != 0));
+                const uint32_t id = make_idesc(128, 128);
+                const uint64_t k_s = k_k + (s & 1) * (TILE / 16);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_P, q_k + k * 2, k_s + k * 2, id, k != 0);
+                if (r.dk > 64)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_P, q_k + BLOCK / 16 + k * 2, k_s + BLOCK / 16 + k * 2, id, 1);
+                tc_commit(BAR(SC));
+                tc_commit(BAR(KE + (s & 1)));
+            };
+            Step st(p, first);
+            if (!STATE_ONLY && steps > 0) scores(0, p.m.role[st.role]);
+            for (int s = 0; s < steps && ok; ++s) {
+                const MixRole &r = p.m.role[st.role];
+                const uint32_t ph = s & 1, nv = r.dv > 64 ? 128 : 64, id_b = make_idesc(128, nv) | (1u << 16), id_ab = id_b | (1u << 15);
+                const uint64_t v_s = v_mn + (s & 1) * (TILE / 16);
+                wait(SR, ph);
+                if (!STATE_ONLY) {
+                    wait(OE, ph ^ 1);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_X, q_k + k * 2, s_mn + k * 128, id_b, k != 0);   // S as it lies: rows of 64 columns of v
+                    if (r.dk > 64)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_X, q_k + BLOCK / 16 + k * 2, s_mn + (4 + k) * 128, id_b, 1);
+                    tc_commit(BAR(QE));
+                }
+                wait(VK + (s & 1), s >> 1 & 1);
+#pragma unroll 1
+                for (int pc = 0; pc < PIECES; ++pc) {
+                    const int slot = pc % SLOTS;
+                    wait(PLF + slot, pc / SLOTS & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int pl = 2; pl >= 0; --pl)   // the smallest first
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            mma_ss(tmem + TM_U, pl_mn + (slot_at(slot) + pl * PLANE) / 16 + k * 128, v_s + (2 * pc + k) * 128, id_ab, (pc != 0) | (pl != 2) | (k != 0));
+                    tc_commit(BAR(PLE + slot));
+                }
+                if (!ok) break;
                 tc_commit(BAR(DSF));
                 if (!STATE_ONLY) {
                     wait(PR, ph);
                     if (!ok) break;
                     tc_fence_after();
-                    for (int k = 0; k < 8; ++k)
-                        mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, make_desc_sw128_mn(base + SM_V + k * 2048, BLOCK), id_b, k != 0);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, v_s + k * 128, id_b, k != 0);
                     tc_commit(BAR(OF));
                 }
-                tc_commit(BAR(VE));
+                if (STATE_ONLY) tc_commit(BAR(VE + (s & 1)));   // else the outputs leave through v's tile first
+                st.next(p);
+                if (!STATE_ONLY && s + 1 < steps) scores(s + 1, p.m.role[st.role]);
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp < P_WARPS) {
-        // ---- scores to weights, outputs: a thread has a row (a token)
-        if (!STATE_ONLY) {
-            const int row = warp * 32 + lane;
-            const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-            int unit = -1, tables = 0;
-            for (int s = 0; s < steps && ok; ++s) {
-                const Step st = step_at(p, first + s);
-                const MixRole &r = p.m.role[st.role];
-                const uint32_t ph = s & 1;
-                const int now = (st.role * p.m.B + st.b) * p.m.H + st.h;
-                if (now != unit) {   // tab[32 + e] = sp decay^e; e < 0 is looked at in the pieces on the diagonal, but not used
-                    // (the old table has been read: the last outputs waited for all four warps' weights)
-                    for (int i = tid; i < 32 + CH; i += P_WARPS * 32) tab[i] = i < 32 ? 0.0f : r.sp * decay_power(p.m.log_decay[st.h], (float)(i - 32));
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(BAR(TB));
-                    ok = warp_wait(BAR(TB), tables++ & 1, spin, abort_flag);
-                    if (!ok) break;
-                    unit = now;
+        // ---- what is no number in v; scores to weights, outputs: a thread has a row (a token)
+        auto look_through = [&](int s, const Step &st) {
+            const MixRole &r = p.m.role[st.role];
+            const uint32_t tile = base + SM_V + (s & 1) * TILE;
+            ok = ok && warp_wait_held(BAR(VF + (s & 1)), s >> 1 & 1, spin, abort_flag);
+            if (!ok) return;
+            const int rounds = r.dv > 64 ? 16 : 8;
+            uint32_t found = 0;
+#pragma unroll 8
+            for (int k = 0; k < rounds; ++k) {
+                const uint4 v = lds128(tile + (k * P_WARPS * 32 + tid) * 16);
+                found |= no_numbers(v.x) | no_numbers(v.y) | no_numbers(v.z) | no_numbers(v.w);
+            }
+            if (found & 0x80008000u) {
+                for (int k = 0; k < rounds; ++k) {
+                    const int at = k * P_WARPS * 32 + tid, vrow = (at >> 3) & 127, column = (at >> 10) * 64 + ((at & 7) ^ (vrow & 7)) * 8;
+                    mend_piece(tile + at * 16, column, (uint32_t)(r.reverse ? CH - 1 - vrow : vrow), bad_base + (s & 7) * 33);
                 }
-                ok = warp_wait(BAR(SC), ph, spin, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                const int own = r.reverse ? P_WARPS - 1 - warp : warp;
+                fence_async_smem();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(VK + (s & 1)));
+        };
+        const int row = warp * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        float ld = 0.0f, d1 = 0.0f, far = 0.0f;
+        Step st(p, first), ahead = st;
+        if (steps > 0) look_through(0, ahead);
+        for (int s = 0; s < steps && ok; ++s, st.next(p)) {
+            ahead.next(p);
+            if (STATE_ONLY) {
+                if (s + 1 < steps) look_through(s + 1, ahead);
+                continue;
+            }
+            const MixRole &r = p.m.role[st.role];
+            const uint32_t ph = s & 1;
+            const bool reverse = r.reverse;
+            const int i = reverse ? CH - 1 - row : row;
+            if (st.fresh) {
+                ld = p.m.log_decay[st.h];
+                d1 = decay_power(ld, 1.0f);
+                far = r.si * decay_power(ld, (float)(i + r.first));
+            }
+            ok = warp_wait_held(BAR(SC), ph, spin, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            // Weights by multiplication, column after column away from the diagonal (so that they run into 0 and not out of infinity); a table
+            // in shared memory would compete with the products' operands for its bandwidth.
+            const int own = reverse ? P_WARPS - 1 - warp : warp;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    const int cw = r.reverse ? 3 - c : c;   // the 32 columns' place in walking order
-                    f32x2 x[8];
-                    uint32_t w[16];
-                    if (cw > own) {
+            for (int c = 0; c < 4; ++c) {
+                const int cw = reverse ? 3 - c : c;   // the 32 columns' place in walking order
+                uint32_t w[16];
+                if (cw > own) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = 0u;
-                    } else {
-                        f32x2 v[16];
-                        tmem_ld32(lanes + TM_P + c * 32, v);
+                    for (int j = 0; j < 16; ++j) w[j] = 0u;
+                } else {
+                    f32x2 v[16];
+                    tmem_ld32(lanes + TM_P + c * 32, v);
+                    if (cw == own) {   // chosen, not multiplied by 0: what is masked may be no number
                         tmem_ld_wait();
-                        const float *t = tab + 32 + (r.reverse ? c * 32 - row : row - c * 32);
-                        if (cw == own) {
+                        float run = r.sp;
+                        if (reverse) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {   // chosen, not multiplied by 0: what is masked may be no number
-                                const float w0 = r.reverse ? t[2 * j] : t[-2 * j], w1 = r.reverse ? t[2 * j + 1] : t[-2 * j - 1];
-                                const int e0 = r.reverse ? c * 32 + 2 * j - row : row - c * 32 - 2 * j, e1 = r.reverse ? e0 + 1 : e0 - 1;
-                                w[j] = pack_bf16(e0 >= 0 ? v[j].x * w0 : 0.0f, e1 >= 0 ? v[j].y * w1 : 0.0f);
+                            for (int j = 0; j < 16; ++j) {
+                                const float a = 2 * j > lane ? run * d1 : run, b = 2 * j + 1 > lane ? a * d1 : a;
+                                w[j] = pack_bf16(2 * j >= lane ? v[j].x * a : 0.0f, 2 * j + 1 >= lane ? v[j].y * b : 0.0f);
+                                run = b;
                             }
-                        } else if (r.reverse) {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[j].x * t[2 * j], v[j].y * t[2 * j + 1]);
                         } else {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[j].x * t[-2 * j], v[j].y * t[-2 * j - 1]);
+                            for (int j = 15; j >= 0; --j) {
+                                const float b = 2 * j + 1 < lane ? run * d1 : run, a = 2 * j < lane ? b * d1 : b;
+                                w[j] = pack_bf16(2 * j <= lane ? v[j].x * a : 0.0f, 2 * j + 1 <= lane ? v[j].y * b : 0.0f);
+                                run = a;
+                            }
+                        }
+                    } else {
+                        const float e = r.sp * decay_power(ld, (float)(reverse ? c * 32 - row : row - c * 32 - 31));
+                        f32x2 run = reverse ? pack2(e, e * d1) : pack2(e * d1, e);
+                        const f32x2 step = pack2(d1 * d1, d1 * d1);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const f32x2 x = mul2(reverse ? v[k] : v[15 - k], run);
+                            const uint32_t both = pack_bf16(x.x, x.y);
+                            if (reverse) w[k] = both;
+                            else w[15 - k] = both;
+                            run = mul2(run, step);
                         }
                     }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
-                    // A forward walk overwrites columns that it has read; a reversed one as well: piece c ends at column 16 c + 15
-                    tmem_st16(lanes + TM_P + c * 16, x);
                 }
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(BAR(PR));
+                f32x2 x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+                // over columns that have been read: piece c ends at column 16 c + 15
+                tmem_st16(lanes + TM_P + c * 16, x);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(PR));
 
-                ok = warp_wait(BAR(OF), ph, spin, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                const int t = st.t0 + row, i = r.reverse ? CH - 1 - row : row;
-                const bool live = t >= 0 && t < p.m.T;
-                const float far = r.si * decay_power(p.m.log_decay[st.h], (float)(i + r.first));
-                const uint8_t *bad = (const uint8_t *)(bad_base + s % 3 * 33);
-                const bool any_bad = *(volatile const uint32_t *)(bad + 128) != 0;
-                __nv_bfloat16 *out = (__nv_bfloat16 *)r.o.p + st.b * r.o.batch + t * r.o.token + (long long)st.h * r.dv;
+            if (s + 1 < steps) look_through(s + 1, ahead);
+            ok = ok && warp_wait_held(BAR(OF), ph, spin, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            const uint8_t *bad = (const uint8_t *)(bad_base + (s & 7) * 33);
+            const bool any_bad = *(volatile const uint32_t *)(bad + 128) != 0;
+            // v's tile has been read: the outputs go through it, 16-byte pieces swizzled as the copies want them
+            const uint32_t stage = base + SM_V + (s & 1) * TILE + warp * 32 * 128;
 #pragma unroll 1
-                for (int c = 0; c < r.dv; c += 32) {
-                    f32x2 y[16], x[16];
-                    tmem_ld32(lanes + TM_Y + c, y);
-                    tmem_ld32(lanes + TM_X + c, x);
-                    tmem_ld_wait();
-                    if (c + 32 >= r.dv && !any_bad) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(BAR(OE));
-                    }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) y[j] = fma2(x[j], pack2(far, far), y[j]);
-                    if (any_bad) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            if (i >= bad[c + 2 * j]) y[j].x = __int_as_float(0x7FC00000);
-                            if (i >= bad[c + 2 * j + 1]) y[j].y = __int_as_float(0x7FC00000);
-                        }
-                    }
-                    if (live) {
-#pragma unroll
-                        for (int h = 0; h < 4; ++h)
-                            if (c + 8 * h < r.dv)
-                                *(uint4 *)(out + c + 8 * h) = make_uint4(pack_bf16(y[4 * h].x, y[4 * h].y), pack_bf16(y[4 * h + 1].x, y[4 * h + 1].y),
-                                                                        pack_bf16(y[4 * h + 2].x, y[4 * h + 2].y), pack_bf16(y[4 * h + 3].x, y[4 * h + 3].y));
-                    }
-                }
-                if (any_bad) {   // the list is read to its end before it may be cleared
+            for (int c = 0; c < r.dv; c += 32) {
+                f32x2 y[16], x[16];
+                tmem_ld32(lanes + TM_Y + c, y);
+                tmem_ld32(lanes + TM_X + c, x);
+                tmem_ld_wait();
+                if (c + 32 >= r.dv) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(BAR(OE));
                 }
+                uint32_t w[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    y[j] = fma2(x[j], pack2(far, far), y[j]);
+                    w[j] = pack_bf16(y[j].x, y[j].y);
+                }
+                if (any_bad) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        if (i >= bad[c + 2 * j]) w[j] = w[j] & 0xFFFF0000u | 0x7FC0u;
+                        if (i >= bad[c + 2 * j + 1]) w[j] = w[j] & 0x0000FFFFu | 0x7FC00000u;
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    sts128(stage + c / 64 * BLOCK + lane * 128 + ((((c & 32) / 8 + h) ^ (lane & 7)) << 4), make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
             }
-            if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
+            fence_async_smem();
+            __syncwarp();
+            const int t0 = st.t0 + warp * 32;
+            if (t0 >= 0) {   // rows behind the last token are cut off by the copy
+                if (lane == 0 && t0 < p.m.T) {
+                    for (int j = 0; j * 64 < r.dv; ++j) tma_store_4d(&p.tm[st.role][3], j * 64, st.h, t0, st.b, stage + j * BLOCK);
+                    bulk_commit();
+                    bulk_wait_read0();
+                }
+            } else {         // the end of a reversed walk: a copy must not start in front of the first token
+                for (int k = lane >> 4; k < 32; k += 2) {
+                    const int c = lane & 15;
+                    if (t0 + k >= 0 && c * 8 < r.dv)
+                        *(uint4 *)((__nv_bfloat16 *)r.o.p + st.b * r.o.batch + (t0 + k) * r.o.token + (long long)st.h * r.dv + c * 8) =
+                            lds128(stage + c / 8 * BLOCK + k * 128 + ((c & 7 ^ k & 7) << 4));
+                }
+                fence_async_smem();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(VE + (s & 1)));
         }
+        if (lane == 0) bulk_wait0();
+        if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     } else {
         // ---- planes of the decayed k, and the state: a thread has row d of S and 64 columns
         const int st_tid = tid - P_WARPS * 32, q = warp & 3, e0 = (warp - P_WARPS) / 4 * 64, d = q * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
-        float S[64];
+        f32x2 S2[32];
+        auto at = [&](int j) -> float & { return j & 1 ? S2[j / 2].y : S2[j / 2].x; };
         auto init_state = [&](const Step &st, long long g) {
             const MixRole &r = p.m.role[st.role];
             const long long mat = (long long)(st.b * p.m.H + st.h) * r.dk * r.dv;
             const float *src = STATE_ONLY ? nullptr : r.s_in;
 #pragma unroll
-            for (int j = 0; j < 64; ++j) S[j] = 0.0f;
+            for (int j = 0; j < 32; ++j) S2[j] = pack2(0.0f, 0.0f);
             if (src && d < r.dk) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
-                    if (e0 + j < r.dv) S[j] = src[mat + (r.turned ? (long long)(e0 + j) * r.dk + d : (long long)d * r.dv + e0 + j)];
+                    if (e0 + j < r.dv) at(j) = src[mat + (r.turned ? (long long)(e0 + j) * r.dk + d : (long long)d * r.dv + e0 + j)];
             }
             if (!STATE_ONLY && st.chunk != 0) {   // the stretches in front of this one, block by block
                 const long long begin = g - st.chunk;
@@ -339,8 +439,8 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const float4 v = l[j * 128];
-                        S[4 * j] = fmaf(f, S[4 * j], v.x); S[4 * j + 1] = fmaf(f, S[4 * j + 1], v.y);
-                        S[4 * j + 2] = fmaf(f, S[4 * j + 2], v.z); S[4 * j + 3] = fmaf(f, S[4 * j + 3], v.w);
+                        S2[2 * j] = fma2(pack2(f, f), S2[2 * j], pack2(v.x, v.y));
+                        S2[2 * j + 1] = fma2(pack2(f, f), S2[2 * j + 1], pack2(v.z, v.w));
                     }
                 }
             }
@@ -351,83 +451,75 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                 const uint32_t row = base + SM_S + (e0 / 64) * BLOCK + d * 128;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    sts128(row + ((j ^ (d & 7)) << 4), make_uint4(pack_bf16(S[8 * j], S[8 * j + 1]), pack_bf16(S[8 * j + 2], S[8 * j + 3]),
-                                                                 pack_bf16(S[8 * j + 4], S[8 * j + 5]), pack_bf16(S[8 * j + 6], S[8 * j + 7])));
+                    sts128(row + ((j ^ (d & 7)) << 4), make_uint4(pack_bf16(S2[4 * j].x, S2[4 * j].y), pack_bf16(S2[4 * j + 1].x, S2[4 * j + 1].y),
+                                                                 pack_bf16(S2[4 * j + 2].x, S2[4 * j + 2].y), pack_bf16(S2[4 * j + 3].x, S2[4 * j + 3].y)));
                 fence_async_smem();
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(SR));
         };
-        int unit = -1, n_tokens = 0;
-        float w[4] = {}, f = 0.0f;   // weights of this thread's rows of k, st_tid / 8 + 32 i; the state's
-        if (steps > 0) {
-            init_state(step_at(p, first), first);
-            hand_over();
-        }
-        for (int s = 0; s < steps && ok; ++s) {
-            const Step st = step_at(p, first + s);
+        float ld = 0.0f;
+        Step st(p, first);
+#pragma unroll 1
+        for (int s = 0; s < steps && ok; ++s, st.next(p)) {
             const MixRole &r = p.m.role[st.role];
             const uint32_t ph = s & 1;
-            const int now = (st.role * p.m.B + st.b) * p.m.H + st.h;
-            uint32_t *bad = bad_base + s % 3 * 33;
-            if (now != unit || st.n != n_tokens) {
-                const float ld = p.m.log_decay[st.h];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = (st_tid >> 3) + 32 * i, j = r.reverse ? CH - 1 - row : row;
-                    w[i] = j < st.n ? decay_power(ld, (float)(st.n - j - r.first)) : 0.0f;
-                }
-                f = decay_power(ld, (float)st.n);
-                unit = now;
-                n_tokens = st.n;
+            uint32_t *bad = bad_base + (s & 7) * 33;
+            if (st.fresh) {
+                ld = p.m.log_decay[st.h];
+                init_state(st, first + s);
             }
-            ok = warp_wait(BAR(KF), ph, spin, abort_flag);
+            hand_over();   // (the last state product is done, and with it the far product and the products out of the ring's slots)
+            ok = warp_wait_held(BAR(KF + ph), s >> 1 & 1, spin, abort_flag);
             if (!ok) break;
-            const int blocks = r.dk > 64 ? 2 : 1;
+            // A thread has the same 16 bytes of two rows, 16 apart; the first 128 threads have columns 0 to 63 of k
+            const bool mine = st_tid < 128 || r.dk > 64;
+            const uint32_t src = base + SM_K + ph * TILE + (st_tid >> 7) * BLOCK + (st_tid & 127) * 16;
+            const uint32_t dst = base + (st_tid >> 7) * (PLANE / 2) + (st_tid & 127) * 16;
+            // the weight of a row, decay^(n - j - first), counted down from piece to piece
+            const int row0 = st_tid >> 3 & 15, e_most = st.n - r.first, back = r.reverse ? 16 : -16;
+            int e = e_most - (r.reverse ? CH - 1 - row0 : row0);
 #pragma unroll 1
-            for (int b = 0; b < blocks; ++b)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = b * (int)(BLOCK / 16) + k * S_WARPS * 32 + st_tid;
-                const uint4 v = lds128(base + SM_K + i * 16);
-                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                uint32_t hi[4], mid[4], lo[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x2 x = mul2(bf2x(in[e]), pack2(w[k], w[k]));
-                    hi[e] = pack_bf16(x.x, x.y);
-                    const f32x2 h = bf2x(hi[e]), y = make_float2(x.x - h.x, x.y - h.y);
-                    mid[e] = pack_bf16(y.x, y.y);
-                    const f32x2 m = bf2x(mid[e]);
-                    lo[e] = pack_bf16(y.x - m.x, y.y - m.y);
+            for (int pc = 0; pc < PIECES; ++pc, e += 2 * back) {
+                const int slot = pc % SLOTS;
+                uint32_t v[8] = {}, hi[8], mid[8], lo[8];
+                if (mine) {
+                    const uint4 v0 = lds128(src + pc * 4096), v1 = lds128(src + pc * 4096 + 2048);
+                    v[0] = v0.x; v[1] = v0.y; v[2] = v0.z; v[3] = v0.w; v[4] = v1.x; v[5] = v1.y; v[6] = v1.z; v[7] = v1.w;
                 }
-                const uint32_t dst = base + SM_PLANES + i * 16;
-                sts128(dst, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-                sts128(dst + 2 * BLOCK, make_uint4(mid[0], mid[1], mid[2], mid[3]));
-                sts128(dst + 4 * BLOCK, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+                auto weight = [&](int x) { return x > e_most - st.n && x <= e_most ? decay_power(ld, (float)x) : 0.0f; };   // tokens of this chunk
+                const float w0 = weight(e), w1 = weight(e + back);
+                f32x2 x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { x[i] = mul2(bf2x(v[i]), i < 4 ? pack2(w0, w0) : pack2(w1, w1)); hi[i] = pack_bf16(x[i].x, x[i].y); }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { const f32x2 h = bf2x(hi[i]); x[i] = make_float2(x[i].x - h.x, x[i].y - h.y); mid[i] = pack_bf16(x[i].x, x[i].y); }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { const f32x2 m = bf2x(mid[i]); lo[i] = pack_bf16(x[i].x - m.x, x[i].y - m.y); }
+                if (!STATE_ONLY && pc == 1) ok = ok && warp_wait_held(BAR(QE), ph, spin, abort_flag);   // the far product has read S
+                ok = ok && warp_wait_held(BAR(PLE + slot), (pc / SLOTS & 1) ^ 1, spin, abort_flag);
+                if (!ok) break;
+                if (mine) {
+                    const uint32_t to = dst + slot_at(slot);
+#pragma unroll
+                    for (int i = 0; i < 8; i += 4) {
+                        sts128(to + i * 512, make_uint4(hi[i], hi[i + 1], hi[i + 2], hi[i + 3]));
+                        sts128(to + i * 512 + PLANE, make_uint4(mid[i], mid[i + 1], mid[i + 2], mid[i + 3]));
+                        sts128(to + i * 512 + 2 * PLANE, make_uint4(lo[i], lo[i + 1], lo[i + 2], lo[i + 3]));
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(BAR(PLF + slot));
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) { mbar_arrive(BAR(PL)); mbar_arrive(BAR(KE)); }
-            ok = warp_wait(BAR(VF), ph, spin, abort_flag);
             if (!ok) break;
-            const int vpieces = (r.dv > 64 ? 2 : 1) * (int)(BLOCK / 16);
-#pragma unroll 4
-            for (int i = st_tid; i < vpieces; i += S_WARPS * 32) {
-                const uint4 v = lds128(base + SM_V + i * 16);
-                if (has_no_number(v.x) || has_no_number(v.y) || has_no_number(v.z) || has_no_number(v.w)) {
-                    const int row = (i >> 3) & 127, column = (i >> 10) * 64 + ((i & 7) ^ (row & 7)) * 8;
-                    mend_piece(base + SM_V + i * 16, column, (uint32_t)(r.reverse ? CH - 1 - row : row), bad);
-                    fence_async_smem();
-                }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(BAR(VK));
+            if (lane == 0) mbar_arrive(BAR(KE + ph));
 
-            ok = warp_wait(BAR(DSF), ph, spin, abort_flag);
+            ok = warp_wait_held(BAR(DSF), ph, spin, abort_flag);
             if (!ok) break;
             tc_fence_after();
+            const float f = decay_power(ld, (float)st.n);
 #pragma unroll
             for (int c = 0; c < 64; c += 32) {
                 f32x2 u[16];
@@ -435,18 +527,18 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                     tmem_ld32(lanes + TM_U + e0 + c, u);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) { S[c + 2 * j] = fmaf(f, S[c + 2 * j], r.su * u[j].x); S[c + 2 * j + 1] = fmaf(f, S[c + 2 * j + 1], r.su * u[j].y); }
+                    for (int j = 0; j < 16; ++j) S2[c / 2 + j] = fma2(pack2(f, f), S2[c / 2 + j], mul2(pack2(r.su, r.su), u[j]));
                 }
             }
             if (*(volatile uint32_t *)(bad + 32)) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
-                    if (((const uint8_t *)bad)[e0 + j] != 255) S[j] = __int_as_float(0x7FC00000);
+                    if (((const uint8_t *)bad)[e0 + j] != 255) at(j) = __int_as_float(0x7FC00000);
             }
-            // The list of the step before this one has been read: the outputs by OE and the states by SR, which this state product waited
-            // for.  It serves again in two steps, whose state product waits for this warp's SR.
-            if (warp == P_WARPS && s > 0) {
-                uint32_t *old = bad_base + (s - 1) % 3 * 33;
+            // The list of two steps ago has been read: by the outputs before they let the last step's go on, by the states before their SR.
+            // It serves again in six steps, long after products that wait for this warp's SR.
+            if (warp == P_WARPS && s > 1) {
+                uint32_t *old = bad_base + (s - 2 & 7) * 33;
                 if (*(volatile uint32_t *)(old + 32)) {
                     old[lane] = 0xFFFFFFFFu;
                     __syncwarp();
@@ -457,19 +549,13 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                 float *dst = r.s_out + (long long)(st.b * p.m.H + st.h) * r.dk * r.dv + (long long)d * r.dv + e0;
 #pragma unroll
                 for (int j = 0; j < 64; j += 4)
-                    if (e0 + j < r.dv) *(float4 *)(dst + j) = make_float4(S[j], S[j + 1], S[j + 2], S[j + 3]);
-            }
-            if (s + 1 < steps) {
-                if (st.chunk == p.chunks - 1) init_state(step_at(p, first + s + 1), first + s + 1);
-                if (!STATE_ONLY) ok = warp_wait(BAR(QE), ph, spin, abort_flag);   // the far product has read S
-                if (!ok) break;
-                hand_over();
+                    if (e0 + j < r.dv) *(float4 *)(dst + j) = make_float4(S2[j / 2].x, S2[j / 2].y, S2[j / 2 + 1].x, S2[j / 2 + 1].y);
             }
         }
         if (STATE_ONLY && steps > 0 && ok) {
             float4 *l = (float4 *)p.local + ((size_t)blockIdx.x * 32 + e0 / 4) * 128 + d;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) l[j * 128] = make_float4(S[4 * j], S[4 * j + 1], S[4 * j + 2], S[4 * j + 3]);
+            for (int j = 0; j < 16; ++j) l[j * 128] = make_float4(S2[2 * j].x, S2[2 * j].y, S2[2 * j + 1].x, S2[2 * j + 1].y);
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     }
@@ -521,13 +607,13 @@ cudaError_t sm100_mix(const MixArgs &a, void *scratch, cudaStream_t st) {
     p.spin_ns = g_spin_limit_ns;
     for (int i = 0; i < a.roles; ++i) {
         const MixRole &r = a.role[i];
-        const MixTensor *t[3] = {&r.q, &r.k, &r.v};
-        for (int j = 0; j < 3; ++j) {
+        const MixTensor *t[4] = {&r.q, &r.k, &r.v, &r.o};
+        for (int j = 0; j < 4; ++j) {
             const uint64_t w = j < 2 ? r.dk : r.dv;
             // an axis of one element has no distance: any valid one
             const uint64_t token = a.T > 1 ? t[j]->token : w * a.H, batch = a.B > 1 ? t[j]->batch : w * a.H;
             const uint64_t dims[4] = {w, (uint64_t)a.H, (uint64_t)a.T, (uint64_t)a.B}, strides[3] = {w * 2, token * 2, batch * 2};
-            const uint32_t box[4] = {64, 1, CH, 1};
+            const uint32_t box[4] = {64, 1, j < 3 ? CH : 32u, 1};   // outputs leave warp by warp
             if (!encode_map16_4d(&p.tm[i][j], t[j]->p, dims, strides, box, true)) return cudaErrorNotSupported;
         }
     }

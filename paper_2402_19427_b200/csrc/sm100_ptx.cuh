@@ -81,6 +81,26 @@ __device__ __forceinline__ bool mbar_wait_spin(uint32_t bar, uint32_t parity, un
 __device__ __forceinline__ bool warp_wait_spin(uint32_t bar, uint32_t parity, unsigned long long limit_ns, volatile int *abort_flag) {
     return __all_sync(0xffffffffu, mbar_wait_spin(bar, parity, limit_ns, abort_flag));
 }
+// Bounded wait of a warp that shares its scheduler with working warps: the hardware holds the thread back for as long as it sees fit (no
+// hint), so that it neither takes issue slots, as a spinning warp does, nor sleeps through the arrival.
+__device__ __forceinline__ bool mbar_wait_held(uint32_t bar, uint32_t parity, unsigned long long limit_ns, volatile int *abort_flag) {
+    uint32_t ok;
+    uint64_t t0 = 0;
+    for (uint32_t n = 0;; ++n) {
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((n & 63u) == 63u) {
+            if (*abort_flag) return false;
+            const uint64_t t = gtimer();
+            if (t0 == 0) t0 = t;
+            else if (t - t0 > limit_ns) return false;
+        }
+    }
+}
+__device__ __forceinline__ bool warp_wait_held(uint32_t bar, uint32_t parity, unsigned long long limit_ns, volatile int *abort_flag) {
+    return __all_sync(0xffffffffu, mbar_wait_held(bar, parity, limit_ns, abort_flag));
+}
 // Bounded wait for something that is normally many microseconds away (a ring slot several stages ahead): the thread sleeps
 // between tests instead of being woken by every barrier event of the CTA.
 __device__ __forceinline__ bool mbar_wait_far(uint32_t bar, uint32_t parity, unsigned long long limit_ns, volatile int *abort_flag) {
@@ -219,6 +239,10 @@ __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *tm) { asm 
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *tm, int c0, int t, int b, uint32_t src_smem) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
                  ::"l"(tm), "r"(c0), "r"(t), "r"(b), "r"(src_smem) : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap *tm, int c0, int c1, int c2, int c3, uint32_t src_smem) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];"
+                 ::"l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(src_smem) : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
