@@ -11,7 +11,7 @@
 // Bound by memory: a chunk of 128 x 128 moves 128 KB, 3.0 us of an SM's share of the measured copy rate; the products take 1.7 us.  One block
 // an SM: 224 KB of q, k (twice), v, S, a ring for the planes of k, and outputs on their way.  Each tile is requested again as soon as its last reader is done: q after the
 // far product, k after the scores and planes, v at the chunk's end.  Warps: four turn P into the operand of the near product (in tensor memory,
-// over the scores), look through v and write the outputs, eight make the planes and keep the state, one copies, one issues.
+// over the scores), look through v and write the outputs, eight keep the state, eight make the planes, one copies, one issues.
 //
 // Blocks share the chunks of all (role, sequence, head) evenly, in order; a block that begins inside a sequence takes the state before it
 // from the sums that a first launch (planes and state product only) leaves for the stretches in front of it.
@@ -27,7 +27,9 @@ namespace {
 using namespace ptx;
 
 constexpr int CH = 128;                          // tokens a chunk
-constexpr int P_WARPS = 4, S_WARPS = 8, THREADS = (P_WARPS + S_WARPS + 2) * 32;
+// Warpgroups of four: weights and outputs, state (two), planes (two), copies and products.  768 threads start with 80 registers each;
+// 88 + 2 x 104 + 2 x 64 + 56 are the same 480.
+constexpr int P_WARPS = 4, S_WARPS = 8, K_WARPS = 8, COPY_WARP = P_WARPS + S_WARPS + K_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (COPY_WARP + 4) * 32;
 constexpr uint32_t BLOCK = 128 * 128;            // 128 rows of 64 bf16
 constexpr int PIECES = 4, SLOTS = 2;             // the planes of k: 32 tokens at a time through two slots
 constexpr uint32_t PLANE = 2 * 32 * 128, SLOT = 3 * PLANE;   // 32 tokens of 2 x 64 values
@@ -94,7 +96,7 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t w) { return (w & 0x7F807
 
 // The values of a 16-byte piece of v that are no numbers become 0 in shared memory: a product would carry them into rows of tokens
 // before theirs, as 0 * NaN.  Byte c of `bad` holds the first token (in walking order) from which on column c is NaN, 255: none.
-__device__ __noinline__ void mend_piece(uint32_t addr, int column, uint32_t token, uint32_t *bad) {
+__device__ __forceinline__ void mend_piece(uint32_t addr, int column, uint32_t token, uint32_t *bad) {
     uint4 v = lds128(addr);
     uint32_t w[4] = {v.x, v.y, v.z, v.w};
     for (int e = 0; e < 8; ++e) {
@@ -128,14 +130,14 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
 
     if (tid == 0) {
         for (int i = 0; i < NBAR; ++i) {
-            const bool by_p = i == PR || i == OE || i == VK || i == VK + 1 || (!STATE_ONLY && (i == VE || i == VE + 1)), to_k = i == KE || i == KE + 1, by_s = i == SR || to_k || (i >= PLF && i < PLE);
-            mbar_init(BAR(i), by_p ? P_WARPS : by_s ? S_WARPS + (to_k && !STATE_ONLY) : 1);
+            const bool by_p = i == PR || i == OE || i == VK || i == VK + 1 || (!STATE_ONLY && (i == VE || i == VE + 1)), to_k = i == KE || i == KE + 1, by_k = to_k || (i >= PLF && i < PLE);
+            mbar_init(BAR(i), by_p ? P_WARPS : i == SR ? S_WARPS : by_k ? K_WARPS + (to_k && !STATE_ONLY) : 1);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid < 8 * 33) bad_base[tid] = tid % 33 == 32 ? 0u : 0xFFFFFFFFu;
-    if (warp == P_WARPS + S_WARPS + 1) { tmem_alloc(smem_u32(tmem_base_s), 512); tmem_relinquish(); }
+    if (warp == MMA_WARP) { tmem_alloc(smem_u32(tmem_base_s), 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -151,7 +153,11 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
     }
     const int steps = (int)(last - first);
 
-    if (warp == P_WARPS + S_WARPS) {
+    // (each role takes its registers in its own branch: behind a join, all code would get by with the fewest)
+    if (warp > MMA_WARP) {
+        reg_dec<56>();
+    } else if (warp == COPY_WARP) {
+        reg_dec<56>();
         // ---- copies: k and v one chunk ahead of q
         if (lane == 0) {
             auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
@@ -178,58 +184,65 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
-    } else if (warp == P_WARPS + S_WARPS + 1) {
+    } else if (warp == MMA_WARP) {
+        reg_dec<56>();
         // ---- products
         // Waits never suspend the thread: what it waits for is tens of cycles away, waking up takes hundreds.
         if (lane == 0) {
             auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); };
-            // descriptors: 16 bytes are one unit of their address field
-            const uint64_t q_k = make_desc_sw128(base + SM_Q), k_k = make_desc_sw128(base + SM_K), v_mn = make_desc_sw128_mn(base + SM_V, BLOCK),
-                           s_mn = make_desc_sw128_mn(base + SM_S, BLOCK), pl_mn = make_desc_sw128_mn(base, PLANE / 2);   // a piece's two blocks of 64 values of k
+            // Descriptors are counted on from step to step (16 bytes are one unit of their address field): held for all steps at once they
+            // would not fit this warpgroup's registers.
+            auto kmajor = [&](uint32_t at) { return make_desc_sw128(base + at); };
+            auto turned = [&](uint32_t at, uint32_t block) { return make_desc_sw128_mn(base + at, block); };
             auto scores = [&](int s, const MixRole &r) {
                 wait(QF, s & 1); wait(KF + (s & 1), s >> 1 & 1);
                 if (!ok) return;
                 tc_fence_after();
                 const uint32_t id = make_idesc(128, 128);
-                const uint64_t k_s = k_k + (s & 1) * (TILE / 16);
+#pragma unroll 1
+                for (int b = 0; b * 64 < r.dk; ++b) {
+                    const uint64_t q = kmajor(SM_Q + b * BLOCK), k = kmajor(SM_K + (s & 1) * TILE + b * BLOCK);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_P, q_k + k * 2, k_s + k * 2, id, k != 0);
-                if (r.dk > 64)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_P, q_k + BLOCK / 16 + k * 2, k_s + BLOCK / 16 + k * 2, id, 1);
+                    for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_P, q + 2 * i, k + 2 * i, id, b | i);
+                }
                 tc_commit(BAR(SC));
                 tc_commit(BAR(KE + (s & 1)));
             };
             Step st(p, first);
             if (!STATE_ONLY && steps > 0) scores(0, p.m.role[st.role]);
+#pragma unroll 1
             for (int s = 0; s < steps && ok; ++s) {
                 const MixRole &r = p.m.role[st.role];
                 const uint32_t ph = s & 1, nv = r.dv > 64 ? 128 : 64, id_b = make_idesc(128, nv) | (1u << 16), id_ab = id_b | (1u << 15);
-                const uint64_t v_s = v_mn + (s & 1) * (TILE / 16);
+                const uint32_t v_at = SM_V + (s & 1) * TILE;
                 wait(SR, ph);
                 if (!STATE_ONLY) {
                     wait(OE, ph ^ 1);
                     if (!ok) break;
                     tc_fence_after();
+                    uint64_t state = turned(SM_S, BLOCK);   // S as it lies: rows of 64 columns of v
+#pragma unroll 1
+                    for (int b = 0; b * 64 < r.dk; ++b, state += 4 * 128) {
+                        const uint64_t q = kmajor(SM_Q + b * BLOCK);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_X, q_k + k * 2, s_mn + k * 128, id_b, k != 0);   // S as it lies: rows of 64 columns of v
-                    if (r.dk > 64)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_ss(tmem + TM_X, q_k + BLOCK / 16 + k * 2, s_mn + (4 + k) * 128, id_b, 1);
+                        for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_X, q + 2 * i, state + 128 * i, id_b, b | i);
+                    }
                     tc_commit(BAR(QE));
                 }
                 wait(VK + (s & 1), s >> 1 & 1);
+                uint64_t v = turned(v_at, BLOCK);
 #pragma unroll 1
-                for (int pc = 0; pc < PIECES; ++pc) {
+                for (int pc = 0; pc < PIECES; ++pc, v += 256) {
                     const int slot = pc % SLOTS;
                     wait(PLF + slot, pc / SLOTS & 1);
                     if (!ok) break;
                     tc_fence_after();
+                    const uint64_t plane = turned(slot_at(slot) + 2 * PLANE, PLANE / 2);   // a piece's two blocks of 64 values of k; the smallest plane first
 #pragma unroll
-                    for (int pl = 2; pl >= 0; --pl)   // the smallest first
-#pragma unroll
-                        for (int k = 0; k < 2; ++k)
-                            mma_ss(tmem + TM_U, pl_mn + (slot_at(slot) + pl * PLANE) / 16 + k * 128, v_s + (2 * pc + k) * 128, id_ab, (pc != 0) | (pl != 2) | (k != 0));
+                    for (int pl = 0; pl < 3; ++pl) {
+                        mma_ss(tmem + TM_U, plane - pl * (PLANE / 16), v, id_ab, pc | pl);
+                        mma_ss(tmem + TM_U, plane - pl * (PLANE / 16) + 128, v + 128, id_ab, 1);
+                    }
                     tc_commit(BAR(PLE + slot));
                 }
                 if (!ok) break;
@@ -238,8 +251,9 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                     wait(PR, ph);
                     if (!ok) break;
                     tc_fence_after();
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, v_s + k * 128, id_b, k != 0);
+                    v = turned(v_at, BLOCK);
+#pragma unroll 4
+                    for (int k = 0; k < 8; ++k) mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, v + k * 128, id_b, k);
                     tc_commit(BAR(OF));
                 }
                 if (STATE_ONLY) tc_commit(BAR(VE + (s & 1)));   // else the outputs leave through v's tile first
@@ -249,6 +263,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp < P_WARPS) {
+        reg_inc<88>();
         // ---- what is no number in v; scores to weights, outputs: a thread has a row (a token)
         auto look_through = [&](int s, const Step &st) {
             const MixRole &r = p.m.role[st.role];
@@ -361,32 +376,32 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             // v's tile has been read: the outputs go through it, 16-byte pieces swizzled as the copies want them
             const uint32_t stage = base + SM_V + (s & 1) * TILE + warp * 32 * 128;
 #pragma unroll 1
-            for (int c = 0; c < r.dv; c += 32) {
-                f32x2 y[16], x[16];
-                tmem_ld32(lanes + TM_Y + c, y);
-                tmem_ld32(lanes + TM_X + c, x);
+            for (int c = 0; c < r.dv; c += 16) {
+                f32x2 y[8], x[8];
+                tmem_ld16(lanes + TM_Y + c, y);
+                tmem_ld16(lanes + TM_X + c, x);
                 tmem_ld_wait();
-                if (c + 32 >= r.dv) {
+                if (c + 16 >= r.dv) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(BAR(OE));
                 }
-                uint32_t w[16];
+                uint32_t w[8];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
+                for (int j = 0; j < 8; ++j) {
                     y[j] = fma2(x[j], pack2(far, far), y[j]);
                     w[j] = pack_bf16(y[j].x, y[j].y);
                 }
                 if (any_bad) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
+                    for (int j = 0; j < 8; ++j) {
                         if (i >= bad[c + 2 * j]) w[j] = w[j] & 0xFFFF0000u | 0x7FC0u;
                         if (i >= bad[c + 2 * j + 1]) w[j] = w[j] & 0x0000FFFFu | 0x7FC00000u;
                     }
                 }
-#pragma unroll
-                for (int h = 0; h < 4; ++h)
-                    sts128(stage + c / 64 * BLOCK + lane * 128 + ((((c & 32) / 8 + h) ^ (lane & 7)) << 4), make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
+                const uint32_t to = stage + c / 64 * BLOCK + lane * 128, piece = c / 8 & 7;
+                sts128(to + ((piece ^ lane & 7) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                sts128(to + ((piece + 1 ^ lane & 7) << 4), make_uint4(w[4], w[5], w[6], w[7]));
             }
             fence_async_smem();
             __syncwarp();
@@ -411,9 +426,10 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         }
         if (lane == 0) bulk_wait0();
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
-    } else {
-        // ---- planes of the decayed k, and the state: a thread has row d of S and 64 columns
-        const int st_tid = tid - P_WARPS * 32, q = warp & 3, e0 = (warp - P_WARPS) / 4 * 64, d = q * 32 + lane;
+    } else if (warp < P_WARPS + S_WARPS) {
+        reg_inc<104>();
+        // ---- the state: a thread has row d of S and 64 columns
+        const int q = warp & 3, e0 = (warp - P_WARPS) / 4 * 64, d = q * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
         f32x2 S2[32];
         auto at = [&](int j) -> float & { return j & 1 ? S2[j / 2].y : S2[j / 2].x; };
@@ -438,6 +454,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                     const float4 *l = (const float4 *)p.local + ((size_t)w * 32 + e0 / 4) * 128 + d;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
+                        if (j % 4 == 0) asm volatile("" ::: "memory");   // four loads at a time: registers
                         const float4 v = l[j * 128];
                         S2[2 * j] = fma2(pack2(f, f), S2[2 * j], pack2(v.x, v.y));
                         S2[2 * j + 1] = fma2(pack2(f, f), S2[2 * j + 1], pack2(v.z, v.w));
@@ -471,63 +488,18 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                 init_state(st, first + s);
             }
             hand_over();   // (the last state product is done, and with it the far product and the products out of the ring's slots)
-            ok = warp_wait_held(BAR(KF + ph), s >> 1 & 1, spin, abort_flag);
-            if (!ok) break;
-            // A thread has the same 16 bytes of two rows, 16 apart; the first 128 threads have columns 0 to 63 of k
-            const bool mine = st_tid < 128 || r.dk > 64;
-            const uint32_t src = base + SM_K + ph * TILE + (st_tid >> 7) * BLOCK + (st_tid & 127) * 16;
-            const uint32_t dst = base + (st_tid >> 7) * (PLANE / 2) + (st_tid & 127) * 16;
-            // the weight of a row, decay^(n - j - first), counted down from piece to piece
-            const int row0 = st_tid >> 3 & 15, e_most = st.n - r.first, back = r.reverse ? 16 : -16;
-            int e = e_most - (r.reverse ? CH - 1 - row0 : row0);
-#pragma unroll 1
-            for (int pc = 0; pc < PIECES; ++pc, e += 2 * back) {
-                const int slot = pc % SLOTS;
-                uint32_t v[8] = {}, hi[8], mid[8], lo[8];
-                if (mine) {
-                    const uint4 v0 = lds128(src + pc * 4096), v1 = lds128(src + pc * 4096 + 2048);
-                    v[0] = v0.x; v[1] = v0.y; v[2] = v0.z; v[3] = v0.w; v[4] = v1.x; v[5] = v1.y; v[6] = v1.z; v[7] = v1.w;
-                }
-                auto weight = [&](int x) { return x > e_most - st.n && x <= e_most ? decay_power(ld, (float)x) : 0.0f; };   // tokens of this chunk
-                const float w0 = weight(e), w1 = weight(e + back);
-                f32x2 x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { x[i] = mul2(bf2x(v[i]), i < 4 ? pack2(w0, w0) : pack2(w1, w1)); hi[i] = pack_bf16(x[i].x, x[i].y); }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { const f32x2 h = bf2x(hi[i]); x[i] = make_float2(x[i].x - h.x, x[i].y - h.y); mid[i] = pack_bf16(x[i].x, x[i].y); }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { const f32x2 m = bf2x(mid[i]); lo[i] = pack_bf16(x[i].x - m.x, x[i].y - m.y); }
-                if (!STATE_ONLY && pc == 1) ok = ok && warp_wait_held(BAR(QE), ph, spin, abort_flag);   // the far product has read S
-                ok = ok && warp_wait_held(BAR(PLE + slot), (pc / SLOTS & 1) ^ 1, spin, abort_flag);
-                if (!ok) break;
-                if (mine) {
-                    const uint32_t to = dst + slot_at(slot);
-#pragma unroll
-                    for (int i = 0; i < 8; i += 4) {
-                        sts128(to + i * 512, make_uint4(hi[i], hi[i + 1], hi[i + 2], hi[i + 3]));
-                        sts128(to + i * 512 + PLANE, make_uint4(mid[i], mid[i + 1], mid[i + 2], mid[i + 3]));
-                        sts128(to + i * 512 + 2 * PLANE, make_uint4(lo[i], lo[i + 1], lo[i + 2], lo[i + 3]));
-                    }
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(BAR(PLF + slot));
-            }
-            if (!ok) break;
-            if (lane == 0) mbar_arrive(BAR(KE + ph));
-
             ok = warp_wait_held(BAR(DSF), ph, spin, abort_flag);
             if (!ok) break;
             tc_fence_after();
             const float f = decay_power(ld, (float)st.n);
 #pragma unroll
-            for (int c = 0; c < 64; c += 32) {
-                f32x2 u[16];
+            for (int c = 0; c < 64; c += 16) {
+                f32x2 u[8];
                 if (e0 + c < r.dv) {
-                    tmem_ld32(lanes + TM_U + e0 + c, u);
+                    tmem_ld16(lanes + TM_U + e0 + c, u);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) S2[c / 2 + j] = fma2(pack2(f, f), S2[c / 2 + j], mul2(pack2(r.su, r.su), u[j]));
+                    for (int j = 0; j < 8; ++j) S2[c / 2 + j] = fma2(pack2(f, f), S2[c / 2 + j], mul2(pack2(r.su, r.su), u[j]));
                 }
             }
             if (*(volatile uint32_t *)(bad + 32)) {
@@ -552,10 +524,65 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                     if (e0 + j < r.dv) *(float4 *)(dst + j) = make_float4(S2[j / 2].x, S2[j / 2].y, S2[j / 2 + 1].x, S2[j / 2 + 1].y);
             }
         }
-        if (STATE_ONLY && steps > 0 && ok) {
+if (STATE_ONLY && steps > 0 && ok) {
             float4 *l = (float4 *)p.local + ((size_t)blockIdx.x * 32 + e0 / 4) * 128 + d;
 #pragma unroll
             for (int j = 0; j < 16; ++j) l[j * 128] = make_float4(S2[2 * j].x, S2[2 * j].y, S2[2 * j + 1].x, S2[2 * j + 1].y);
+        }
+        if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
+    } else {
+        reg_dec<64>();
+        // ---- planes of the decayed k
+        const int k_tid = tid - (P_WARPS + S_WARPS) * 32;
+        float ld = 0.0f;
+        Step st(p, first);
+#pragma unroll 1
+        for (int s = 0; s < steps && ok; ++s, st.next(p)) {
+            const MixRole &r = p.m.role[st.role];
+            const uint32_t ph = s & 1;
+            if (st.fresh) ld = p.m.log_decay[st.h];
+            ok = warp_wait_held(BAR(KF + ph), s >> 1 & 1, spin, abort_flag);
+            if (!ok) break;
+            // A thread has the same 16 bytes of two rows, 16 apart; the first 128 threads have columns 0 to 63 of k
+            const bool mine = k_tid < 128 || r.dk > 64;
+            const uint32_t src = base + SM_K + ph * TILE + (k_tid >> 7) * BLOCK + (k_tid & 127) * 16;
+            const uint32_t dst = base + (k_tid >> 7) * (PLANE / 2) + (k_tid & 127) * 16;
+            // the weight of a row, decay^(n - j - first), counted down from piece to piece
+            const int row0 = k_tid >> 3 & 15, e_most = st.n - r.first, back = r.reverse ? 16 : -16;
+            int e = e_most - (r.reverse ? CH - 1 - row0 : row0);
+#pragma unroll 1
+            for (int pc = 0; pc < PIECES; ++pc, e += 2 * back) {
+                const int slot = pc % SLOTS;
+                auto weight = [&](int x) { return x > e_most - st.n && x <= e_most ? decay_power(ld, (float)x) : 0.0f; };   // tokens of this chunk
+                const float w0 = weight(e), w1 = weight(e + back);
+                if (!STATE_ONLY && pc == 1) ok = warp_wait_held(BAR(QE), ph, spin, abort_flag);   // the far product has read S
+                ok = ok && warp_wait_held(BAR(PLE + slot), (pc / SLOTS & 1) ^ 1, spin, abort_flag);
+                if (!ok) break;
+                if (mine) {
+                    const uint4 v0 = lds128(src + pc * 4096), v1 = lds128(src + pc * 4096 + 2048);
+                    const uint32_t v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+                    uint32_t hi[8], mid[8], lo[8];
+                    f32x2 x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { x[i] = mul2(bf2x(v[i]), i < 4 ? pack2(w0, w0) : pack2(w1, w1)); hi[i] = pack_bf16(x[i].x, x[i].y); }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { const f32x2 h = bf2x(hi[i]); x[i] = make_float2(x[i].x - h.x, x[i].y - h.y); mid[i] = pack_bf16(x[i].x, x[i].y); }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { const f32x2 m = bf2x(mid[i]); lo[i] = pack_bf16(x[i].x - m.x, x[i].y - m.y); }
+                    const uint32_t to = dst + slot_at(slot);
+#pragma unroll
+                    for (int i = 0; i < 8; i += 4) {
+                        sts128(to + i * 512, make_uint4(hi[i], hi[i + 1], hi[i + 2], hi[i + 3]));
+                        sts128(to + i * 512 + PLANE, make_uint4(mid[i], mid[i + 1], mid[i + 2], mid[i + 3]));
+                        sts128(to + i * 512 + 2 * PLANE, make_uint4(lo[i], lo[i + 1], lo[i + 2], lo[i + 3]));
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(BAR(PLF + slot));
+            }
+            if (!ok) break;
+            if (lane == 0) mbar_arrive(BAR(KE + ph));
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     }
@@ -566,7 +593,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == P_WARPS + S_WARPS + 1) tmem_dealloc(tmem, 512);
+    if (warp == MMA_WARP) tmem_dealloc(tmem, 512);
 }
 
 // Blocks: one a (role, sequence, head) while that is as fast, else 148 with equal shares.  In chunks: a block's own, and for cut
