@@ -28,19 +28,20 @@ using namespace ptx;
 
 constexpr int CH = 128;                          // tokens a chunk
 // Warpgroups of four: weights and outputs, state (two), planes (two), copies and products.  768 threads start with 80 registers each;
-// 88 + 2 x 104 + 2 x 64 + 56 are the same 480.
+// 96 + 2 x 120 + 2 x 48 + 48 are the same 480.
 constexpr int P_WARPS = 4, S_WARPS = 8, K_WARPS = 8, COPY_WARP = P_WARPS + S_WARPS + K_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (COPY_WARP + 4) * 32;
 constexpr uint32_t BLOCK = 128 * 128;            // 128 rows of 64 bf16
-constexpr int PIECES = 4, SLOTS = 2;             // the planes of k: 32 tokens at a time through two slots
-constexpr uint32_t PLANE = 2 * 32 * 128, SLOT = 3 * PLANE;   // 32 tokens of 2 x 64 values
+// The planes of the decayed k are made 32 tokens (a piece) at a time.  The first plane takes the place of the k it is made from; the others
+// of pieces 0 and 1 have slots of their own, those of pieces 2 and 3 lie in S's place, which is free from the far product to the next S.
+constexpr int PIECES = 4;
+constexpr uint32_t PLANE = 2 * 32 * 128, SLOT = 2 * PLANE;   // 32 tokens of 2 x 64 values
 constexpr uint32_t TILE = 2 * BLOCK;
-constexpr uint32_t SM_Q = 0, SM_K = TILE, SM_V = SM_K + 2 * TILE, SM_S = SM_V + 2 * TILE, SM_PLANES = SM_S + TILE, SM_BAR = SM_PLANES + SLOT;
-enum { QF, QE, SC, PR, DSF, SR, OF, OE, KF, KE = KF + 2, VF = KE + 2, VK = VF + 2, VE = VK + 2, PLF = VE + 2, PLE = PLF + SLOTS, NBAR = PLE + SLOTS };   // two of each for the two tiles of k and v
+constexpr uint32_t SM_Q = 0, SM_K = TILE, SM_V = SM_K + 2 * TILE, SM_S = SM_V + 2 * TILE, SM_PLANES = SM_S + TILE, SM_BAR = SM_PLANES + 2 * SLOT;
+__host__ __device__ constexpr uint32_t slot_at(int piece) { return piece < 2 ? SM_PLANES + piece * SLOT : SM_S + (piece - 2) * SLOT; }
+static_assert(2 * SLOT <= TILE, "slots in S's place");
+enum { QF, QE, SC, PR, DSF, SR, OF, OE, KF, KE = KF + 2, VF = KE + 2, VK = VF + 2, VE = VK + 2, PLF = VE + 2, NBAR = PLF + PIECES };   // two of each for the two tiles of k and v
 constexpr uint32_t SM_TMEM = SM_BAR + NBAR * 8, SM_BAD = SM_TMEM + 16,
                    SM_TOTAL = SM_BAD + 8 * 132, SM_ALLOC = SM_TOTAL + 1024;
-// The second slot lies in S's place, which is free from the far product to the next S
-__host__ __device__ constexpr uint32_t slot_at(int slot) { return slot == 0 ? SM_PLANES : SM_S; }
-static_assert(SLOT <= TILE, "a slot in S's place");
 static_assert(SM_ALLOC <= 232448, "shared memory of a block");
 constexpr uint32_t TM_P = 0, TM_Y = 128, TM_X = 256, TM_U = 384;   // tensor-memory columns
 constexpr int WALKERS = 148;                     // the plan, and with it the workspace, does not depend on the device
@@ -94,6 +95,8 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
 // Bits 15 and 31 of the result: whether the two bf16 of w are infinite or NaN (all bits of the exponent set)
 __device__ __forceinline__ uint32_t no_numbers(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
 
+// the upper 16 bits of two fp32 values: cut to bf16
+__device__ __forceinline__ uint32_t upper_halves(f32x2 x) { return __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632); }
 // The values of a 16-byte piece of v that are no numbers become 0 in shared memory: a product would carry them into rows of tokens
 // before theirs, as 0 * NaN.  Byte c of `bad` holds the first token (in walking order) from which on column c is NaN, 255: none.
 __device__ __forceinline__ void mend_piece(uint32_t addr, int column, uint32_t token, uint32_t *bad) {
@@ -130,8 +133,8 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
 
     if (tid == 0) {
         for (int i = 0; i < NBAR; ++i) {
-            const bool by_p = i == PR || i == OE || i == VK || i == VK + 1 || (!STATE_ONLY && (i == VE || i == VE + 1)), to_k = i == KE || i == KE + 1, by_k = to_k || (i >= PLF && i < PLE);
-            mbar_init(BAR(i), by_p ? P_WARPS : i == SR ? S_WARPS : by_k ? K_WARPS + (to_k && !STATE_ONLY) : 1);
+            const bool by_p = i == PR || i == OE || i == VK || i == VK + 1 || (!STATE_ONLY && (i == VE || i == VE + 1));
+            mbar_init(BAR(i), by_p ? P_WARPS : i == SR ? S_WARPS : i >= PLF ? K_WARPS : 1);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -155,9 +158,9 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
 
     // (each role takes its registers in its own branch: behind a join, all code would get by with the fewest)
     if (warp > MMA_WARP) {
-        reg_dec<56>();
+        reg_dec<48>();
     } else if (warp == COPY_WARP) {
-        reg_dec<56>();
+        reg_dec<48>();
         // ---- copies: k and v one chunk ahead of q
         if (lane == 0) {
             auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
@@ -185,7 +188,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp == MMA_WARP) {
-        reg_dec<56>();
+        reg_dec<48>();
         // ---- products
         // Waits never suspend the thread: what it waits for is tens of cycles away, waking up takes hundreds.
         if (lane == 0) {
@@ -206,7 +209,6 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                     for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_P, q + 2 * i, k + 2 * i, id, b | i);
                 }
                 tc_commit(BAR(SC));
-                tc_commit(BAR(KE + (s & 1)));
             };
             Step st(p, first);
             if (!STATE_ONLY && steps > 0) scores(0, p.m.role[st.role]);
@@ -215,38 +217,43 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                 const MixRole &r = p.m.role[st.role];
                 const uint32_t ph = s & 1, nv = r.dv > 64 ? 128 : 64, id_b = make_idesc(128, nv) | (1u << 16), id_ab = id_b | (1u << 15);
                 const uint32_t v_at = SM_V + (s & 1) * TILE;
-                wait(SR, ph);
-                if (!STATE_ONLY) {
-                    wait(OE, ph ^ 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    uint64_t state = turned(SM_S, BLOCK);   // S as it lies: rows of 64 columns of v
-#pragma unroll 1
-                    for (int b = 0; b * 64 < r.dk; ++b, state += 4 * 128) {
-                        const uint64_t q = kmajor(SM_Q + b * BLOCK);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_X, q + 2 * i, state + 128 * i, id_b, b | i);
-                    }
-                    tc_commit(BAR(QE));
-                }
-                wait(VK + (s & 1), s >> 1 & 1);
                 uint64_t v = turned(v_at, BLOCK);
-#pragma unroll 1
-                for (int pc = 0; pc < PIECES; ++pc, v += 256) {
-                    const int slot = pc % SLOTS;
-                    wait(PLF + slot, pc / SLOTS & 1);
-                    if (!ok) break;
+                auto piece = [&](int pc) {
+                    wait(PLF + pc, ph);
+                    if (!ok) return;
                     tc_fence_after();
-                    const uint64_t plane = turned(slot_at(slot) + 2 * PLANE, PLANE / 2);   // a piece's two blocks of 64 values of k; the smallest plane first
+                    const uint64_t first_plane = turned(SM_K + (s & 1) * TILE + pc * 4096, BLOCK), others = turned(slot_at(pc), PLANE / 2);
 #pragma unroll
-                    for (int pl = 0; pl < 3; ++pl) {
-                        mma_ss(tmem + TM_U, plane - pl * (PLANE / 16), v, id_ab, pc | pl);
-                        mma_ss(tmem + TM_U, plane - pl * (PLANE / 16) + 128, v + 128, id_ab, 1);
+                    for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, others + PLANE / 16 + k * 128, v + k * 128, id_ab, pc | k);   // the smallest first
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, others + k * 128, v + k * 128, id_ab, 1);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, first_plane + k * 128, v + k * 128, id_ab, 1);
+                    v += 256;
+                };
+                wait(SR, ph);
+                wait(VK + (s & 1), s >> 1 & 1);
+#pragma unroll 1
+                for (int pc = 0; pc < PIECES; ++pc) {
+                    if (!STATE_ONLY && pc == 1) {   // the last outputs have been read by now
+                        wait(OE, ph ^ 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        uint64_t state = turned(SM_S, BLOCK);   // S as it lies: rows of 64 columns of v
+#pragma unroll 1
+                        for (int b = 0; b * 64 < r.dk; ++b, state += 4 * 128) {
+                            const uint64_t q = kmajor(SM_Q + b * BLOCK);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_X, q + 2 * i, state + 128 * i, id_b, b | i);
+                        }
+                        tc_commit(BAR(QE));
                     }
-                    tc_commit(BAR(PLE + slot));
+                    piece(pc);
+                    if (!ok) break;
                 }
                 if (!ok) break;
                 tc_commit(BAR(DSF));
+                tc_commit(BAR(KE + (s & 1)));
                 if (!STATE_ONLY) {
                     wait(PR, ph);
                     if (!ok) break;
@@ -263,7 +270,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp < P_WARPS) {
-        reg_inc<88>();
+        reg_inc<96>();
         // ---- what is no number in v; scores to weights, outputs: a thread has a row (a token)
         auto look_through = [&](int s, const Step &st) {
             const MixRole &r = p.m.role[st.role];
@@ -376,32 +383,32 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             // v's tile has been read: the outputs go through it, 16-byte pieces swizzled as the copies want them
             const uint32_t stage = base + SM_V + (s & 1) * TILE + warp * 32 * 128;
 #pragma unroll 1
-            for (int c = 0; c < r.dv; c += 16) {
-                f32x2 y[8], x[8];
-                tmem_ld16(lanes + TM_Y + c, y);
-                tmem_ld16(lanes + TM_X + c, x);
+            for (int c = 0; c < r.dv; c += 32) {
+                f32x2 y[16], x[16];
+                tmem_ld32(lanes + TM_Y + c, y);
+                tmem_ld32(lanes + TM_X + c, x);
                 tmem_ld_wait();
-                if (c + 16 >= r.dv) {
+                if (c + 32 >= r.dv) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(BAR(OE));
                 }
-                uint32_t w[8];
+                uint32_t w[16];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < 16; ++j) {
                     y[j] = fma2(x[j], pack2(far, far), y[j]);
                     w[j] = pack_bf16(y[j].x, y[j].y);
                 }
                 if (any_bad) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < 16; ++j) {
                         if (i >= bad[c + 2 * j]) w[j] = w[j] & 0xFFFF0000u | 0x7FC0u;
                         if (i >= bad[c + 2 * j + 1]) w[j] = w[j] & 0x0000FFFFu | 0x7FC00000u;
                     }
                 }
-                const uint32_t to = stage + c / 64 * BLOCK + lane * 128, piece = c / 8 & 7;
-                sts128(to + ((piece ^ lane & 7) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-                sts128(to + ((piece + 1 ^ lane & 7) << 4), make_uint4(w[4], w[5], w[6], w[7]));
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    sts128(stage + c / 64 * BLOCK + lane * 128 + ((((c & 32) / 8 + h) ^ (lane & 7)) << 4), make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
             }
             fence_async_smem();
             __syncwarp();
@@ -427,7 +434,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         if (lane == 0) bulk_wait0();
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     } else if (warp < P_WARPS + S_WARPS) {
-        reg_inc<104>();
+        reg_inc<120>();
         // ---- the state: a thread has row d of S and 64 columns
         const int q = warp & 3, e0 = (warp - P_WARPS) / 4 * 64, d = q * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
@@ -462,16 +469,17 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                 }
             }
         };
-        // S to shared memory for the far product: rows of 64 columns, 16-byte pieces swizzled as a tiled copy would have them
-        auto hand_over = [&]() {
-            if (!STATE_ONLY) {
-                const uint32_t row = base + SM_S + (e0 / 64) * BLOCK + d * 128;
+        // S to shared memory for the far product: rows of 64 columns, 16-byte pieces swizzled as a tiled copy would have them; sixteen
+        // columns at a time
+        const uint32_t s_row = base + SM_S + (e0 / 64) * BLOCK + d * 128;
+        auto put16 = [&](int c) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    sts128(row + ((j ^ (d & 7)) << 4), make_uint4(pack_bf16(S2[4 * j].x, S2[4 * j].y), pack_bf16(S2[4 * j + 1].x, S2[4 * j + 1].y),
-                                                                 pack_bf16(S2[4 * j + 2].x, S2[4 * j + 2].y), pack_bf16(S2[4 * j + 3].x, S2[4 * j + 3].y)));
-                fence_async_smem();
-            }
+            for (int j = c / 8; j < c / 8 + 2; ++j)
+                sts128(s_row + ((j ^ (d & 7)) << 4), make_uint4(pack_bf16(S2[4 * j].x, S2[4 * j].y), pack_bf16(S2[4 * j + 1].x, S2[4 * j + 1].y),
+                                                               pack_bf16(S2[4 * j + 2].x, S2[4 * j + 2].y), pack_bf16(S2[4 * j + 3].x, S2[4 * j + 3].y)));
+        };
+        auto handed_over = [&]() {
+            if (!STATE_ONLY) fence_async_smem();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(SR));
@@ -486,27 +494,39 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             if (st.fresh) {
                 ld = p.m.log_decay[st.h];
                 init_state(st, first + s);
+                if (!STATE_ONLY)
+#pragma unroll
+                    for (int c = 0; c < 64; c += 16) put16(c);
+                handed_over();
             }
-            hand_over();   // (the last state product is done, and with it the far product and the products out of the ring's slots)
+            const float f = decay_power(ld, (float)st.n), su = r.su;
+            const bool last_chunk = st.chunk == p.chunks - 1;
+            const int columns = r.dv - e0;
             ok = warp_wait_held(BAR(DSF), ph, spin, abort_flag);
             if (!ok) break;
             tc_fence_after();
-            const float f = decay_power(ld, (float)st.n);
+            // The state product is done, and with it the far product and the products out of the second slot: S may be overwritten
+            f32x2 u[2][8];
+            tmem_ld16(lanes + TM_U + e0, u[0]);
 #pragma unroll
             for (int c = 0; c < 64; c += 16) {
-                f32x2 u[8];
-                if (e0 + c < r.dv) {
-                    tmem_ld16(lanes + TM_U + e0 + c, u);
-                    tmem_ld_wait();
+                tmem_ld_wait();
+                if (c + 16 < 64) tmem_ld16(lanes + TM_U + e0 + c + 16, u[c / 16 + 1 & 1]);
+                if (c < columns) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) S2[c / 2 + j] = fma2(pack2(f, f), S2[c / 2 + j], mul2(pack2(r.su, r.su), u[j]));
+                    for (int j = 0; j < 8; ++j) S2[c / 2 + j] = fma2(pack2(f, f), S2[c / 2 + j], mul2(pack2(su, su), u[c / 16 & 1][j]));
                 }
+                if (!STATE_ONLY && !last_chunk) put16(c);
             }
             if (*(volatile uint32_t *)(bad + 32)) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
                     if (((const uint8_t *)bad)[e0 + j] != 255) at(j) = __int_as_float(0x7FC00000);
+                if (!STATE_ONLY && !last_chunk)
+#pragma unroll
+                    for (int c = 0; c < 64; c += 16) put16(c);
             }
+            if (!last_chunk) handed_over();
             // The list of two steps ago has been read: by the outputs before they let the last step's go on, by the states before their SR.
             // It serves again in six steps, long after products that wait for this warp's SR.
             if (warp == P_WARPS && s > 1) {
@@ -517,7 +537,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                     if (lane == 0) old[32] = 0u;
                 }
             }
-            if (!STATE_ONLY && st.chunk == p.chunks - 1 && r.s_out && d < r.dk) {
+            if (!STATE_ONLY && last_chunk && r.s_out && d < r.dk) {
                 float *dst = r.s_out + (long long)(st.b * p.m.H + st.h) * r.dk * r.dv + (long long)d * r.dv + e0;
 #pragma unroll
                 for (int j = 0; j < 64; j += 4)
@@ -531,58 +551,65 @@ if (STATE_ONLY && steps > 0 && ok) {
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     } else {
-        reg_dec<64>();
+        reg_dec<48>();
         // ---- planes of the decayed k
         const int k_tid = tid - (P_WARPS + S_WARPS) * 32;
-        float ld = 0.0f;
+        float weight = 0.0f;
+        int n_tokens = 0;
         Step st(p, first);
 #pragma unroll 1
         for (int s = 0; s < steps && ok; ++s, st.next(p)) {
             const MixRole &r = p.m.role[st.role];
             const uint32_t ph = s & 1;
-            if (st.fresh) ld = p.m.log_decay[st.h];
+            if (st.fresh || st.n != n_tokens) {   // lane (8 i + m) of a warp: the weight decay^(n - j - first) of the warp's row i + 16 m
+                const int row = (k_tid >> 3 & 15) + 16 * (lane & 7), j = r.reverse ? CH - 1 - row : row;
+                weight = j < st.n ? decay_power(p.m.log_decay[st.h], (float)(st.n - j - r.first)) : 0.0f;
+                n_tokens = st.n;
+            }
             ok = warp_wait_held(BAR(KF + ph), s >> 1 & 1, spin, abort_flag);
             if (!ok) break;
             // A thread has the same 16 bytes of two rows, 16 apart; the first 128 threads have columns 0 to 63 of k
             const bool mine = k_tid < 128 || r.dk > 64;
             const uint32_t src = base + SM_K + ph * TILE + (k_tid >> 7) * BLOCK + (k_tid & 127) * 16;
             const uint32_t dst = base + (k_tid >> 7) * (PLANE / 2) + (k_tid & 127) * 16;
-            // the weight of a row, decay^(n - j - first), counted down from piece to piece
-            const int row0 = k_tid >> 3 & 15, e_most = st.n - r.first, back = r.reverse ? 16 : -16;
-            int e = e_most - (r.reverse ? CH - 1 - row0 : row0);
 #pragma unroll 1
-            for (int pc = 0; pc < PIECES; ++pc, e += 2 * back) {
-                const int slot = pc % SLOTS;
-                auto weight = [&](int x) { return x > e_most - st.n && x <= e_most ? decay_power(ld, (float)x) : 0.0f; };   // tokens of this chunk
-                const float w0 = weight(e), w1 = weight(e + back);
-                if (!STATE_ONLY && pc == 1) ok = warp_wait_held(BAR(QE), ph, spin, abort_flag);   // the far product has read S
-                ok = ok && warp_wait_held(BAR(PLE + slot), (pc / SLOTS & 1) ^ 1, spin, abort_flag);
-                if (!ok) break;
+            for (int pc = 0; pc < PIECES; ++pc) {
+                const float w0 = __shfl_sync(0xffffffffu, weight, (lane & 24) + 2 * pc), w1 = __shfl_sync(0xffffffffu, weight, (lane & 24) + 2 * pc + 1);
+                uint32_t v[8] = {}, hi[8], mid[8], lo[8];
                 if (mine) {
                     const uint4 v0 = lds128(src + pc * 4096), v1 = lds128(src + pc * 4096 + 2048);
-                    const uint32_t v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-                    uint32_t hi[8], mid[8], lo[8];
-                    f32x2 x[8];
+                    v[0] = v0.x; v[1] = v0.y; v[2] = v0.z; v[3] = v0.w; v[4] = v1.x; v[5] = v1.y; v[6] = v1.z; v[7] = v1.w;
+                }
+                // cut, not rounded: 24 bits are three times eight, so the three add up to the product exactly
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) { x[i] = mul2(bf2x(v[i]), i < 4 ? pack2(w0, w0) : pack2(w1, w1)); hi[i] = pack_bf16(x[i].x, x[i].y); }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { const f32x2 h = bf2x(hi[i]); x[i] = make_float2(x[i].x - h.x, x[i].y - h.y); mid[i] = pack_bf16(x[i].x, x[i].y); }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { const f32x2 m = bf2x(mid[i]); lo[i] = pack_bf16(x[i].x - m.x, x[i].y - m.y); }
-                    const uint32_t to = dst + slot_at(slot);
+                for (int i = 0; i < 8; ++i) {
+                    const f32x2 minus = pack2(-1.0f, -1.0f);
+                    f32x2 x = mul2(bf2x(v[i]), i < 4 ? pack2(w0, w0) : pack2(w1, w1));
+                    hi[i] = upper_halves(x);
+                    x = fma2(bf2x(hi[i]), minus, x);
+                    mid[i] = upper_halves(x);
+                    x = fma2(bf2x(mid[i]), minus, x);
+                    lo[i] = upper_halves(x);
+                }
+                if (pc == 0) {   // the last state product has read the slots, the scores k
+                    ok = warp_wait_held(BAR(DSF), ph ^ 1, spin, abort_flag);
+                    if (!STATE_ONLY) ok = ok && warp_wait_held(BAR(SC), ph, spin, abort_flag);
+                }
+                if (!STATE_ONLY && pc == 2) ok = warp_wait_held(BAR(QE), ph, spin, abort_flag);   // the far product has read S
+                if (!ok) break;
+                if (mine) {
+                    const uint32_t to = dst + slot_at(pc);
 #pragma unroll
                     for (int i = 0; i < 8; i += 4) {
-                        sts128(to + i * 512, make_uint4(hi[i], hi[i + 1], hi[i + 2], hi[i + 3]));
-                        sts128(to + i * 512 + PLANE, make_uint4(mid[i], mid[i + 1], mid[i + 2], mid[i + 3]));
-                        sts128(to + i * 512 + 2 * PLANE, make_uint4(lo[i], lo[i + 1], lo[i + 2], lo[i + 3]));
+                        sts128(src + pc * 4096 + i * 512, make_uint4(hi[i], hi[i + 1], hi[i + 2], hi[i + 3]));
+                        sts128(to + i * 512, make_uint4(mid[i], mid[i + 1], mid[i + 2], mid[i + 3]));
+                        sts128(to + i * 512 + PLANE, make_uint4(lo[i], lo[i + 1], lo[i + 2], lo[i + 3]));
                     }
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(BAR(PLF + slot));
+                if (lane == 0) mbar_arrive(BAR(PLF + pc));
             }
-            if (!ok) break;
-            if (lane == 0) mbar_arrive(BAR(KE + ph));
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     }
