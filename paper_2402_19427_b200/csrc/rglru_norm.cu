@@ -5,8 +5,8 @@
 //
 // Both are bound by memory: 4 bytes an element forward, 6 backward (bf16).  A row is read once and stays in registers between the
 // statistics and the result, so that the deviations are taken from the mean itself (no difference of large sums).  A group of threads owns a
-// row: up to a warp of them for narrow rows, several rows a warp; a whole block for wide ones.  Groups walk rows with the next row's
-// loads in flight and the weights in registers.
+// row: up to a warp of them for narrow rows, several rows a warp; a whole block for wide ones.  The
+// backward's groups walk rows with the next row's loads in flight, the weights and the columns' sums in registers.
 #include <cuda_bf16.h>
 
 #include "rglru_internal.h"
@@ -30,55 +30,61 @@ struct NormArgs {
     float *part;         // backward: [blocks][2][N] sums of dy xh and dy over a block's rows, or null
 };
 
-// VE neighbouring elements as they lie in memory
-template <typename IO, int VE> struct Raw { uint32_t w[VE * sizeof(IO) / 4]; };
-template <> struct Raw<__nv_bfloat16, 1> { uint16_t w; };
+// VE neighbouring elements as they lie in memory: 2, 4, 8 or 16 bytes
+template <int BYTES> struct Word { using type = uint4; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<2> { using type = uint16_t; };
+template <typename IO, int VE> using Raw = typename Word<VE * (int)sizeof(IO)>::type;
 
-template <typename IO, int VE> __device__ __forceinline__ Raw<IO, VE> load_raw(const IO *p) {
-    Raw<IO, VE> r;
-    if constexpr (VE * sizeof(IO) == 16) {
-        const uint4 v = *(const uint4 *)p;
-        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
-    } else if constexpr (sizeof(IO) == 4) {
-        r.w[0] = *(const uint32_t *)p;
-    } else {
-        r.w = *(const uint16_t *)p;
-    }
-    return r;
-}
+template <typename IO, int VE> __device__ __forceinline__ Raw<IO, VE> load_raw(const IO *p) { return *(const Raw<IO, VE> *)p; }
 template <typename IO, int VE> __device__ __forceinline__ void unpack(const Raw<IO, VE> &r, float (&f)[VE]) {
-    if constexpr (sizeof(IO) == 4) {
-#pragma unroll
-        for (int e = 0; e < VE; ++e) f[e] = __uint_as_float(r.w[e]);
-    } else if constexpr (VE == 1) {
-        f[0] = __uint_as_float((uint32_t)r.w << 16);
+    if constexpr (sizeof(r) == 2) {
+        f[0] = __uint_as_float((uint32_t)r << 16);
     } else {
+        constexpr int W = sizeof(r) / 4;
+        uint32_t w[W];
+        if constexpr (W == 1) w[0] = r;
+        else if constexpr (W == 2) { w[0] = r.x; w[1] = r.y; }
+        else { w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w; }
 #pragma unroll
-        for (int e = 0; e < VE; e += 2) { const f32x2 v = bf2x(r.w[e / 2]); f[e] = v.x; f[e + 1] = v.y; }
+        for (int i = 0; i < W; ++i) {
+            if constexpr (sizeof(IO) == 4) f[i] = __uint_as_float(w[i]);
+            else { const f32x2 v = bf2x(w[i]); f[2 * i] = v.x; f[2 * i + 1] = v.y; }
+        }
     }
 }
 template <typename IO, int VE> __device__ __forceinline__ void store_vec(IO *p, const float (&f)[VE]) {
-    if constexpr (VE == 1) {
-        if constexpr (sizeof(IO) == 4) *p = f[0];
-        else *p = __float2bfloat16_rn(f[0]);
-    } else if constexpr (sizeof(IO) == 4) {
-        *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+    if constexpr (VE * sizeof(IO) == 2) {
+        *p = __float2bfloat16_rn(f[0]);
     } else {
-        *(uint4 *)p = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+        constexpr int W = VE * sizeof(IO) / 4;
+        uint32_t w[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (sizeof(IO) == 4) w[i] = __float_as_uint(f[i]);
+            else w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+        }
+        if constexpr (W == 1) *(uint32_t *)p = w[0];
+        else if constexpr (W == 2) *(uint2 *)p = make_uint2(w[0], w[1]);
+        else
+#pragma unroll
+            for (int i = 0; i < W; i += 4) *((uint4 *)p + i / 4) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
     }
 }
 template <int VE> __device__ __forceinline__ void load_f32(const float *p, float (&f)[VE]) {
 #pragma unroll
-    for (int e = 0; e < VE; e += (VE % 4 == 0 ? 4 : 1)) {
+    for (int e = 0; e < VE; e += (VE % 4 == 0 ? 4 : VE)) {
         if constexpr (VE % 4 == 0) { const float4 v = *(const float4 *)(p + e); f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w; }
+        else if constexpr (VE == 2) { const float2 v = *(const float2 *)p; f[0] = v.x; f[1] = v.y; }
         else f[e] = p[e];
     }
 }
 
-// Sums of K values over the group of threads that owns a row; every thread of the group gets them.  Wide groups go through
-// shared memory, in two buffers used in turn, so that one barrier per call is enough.
+// Sums of K values over the group of threads that owns a row; every thread of the group gets them.  Wide groups leave their warps' sums in
+// shared memory, in two buffers used in turn, so that one barrier a call is enough, and every thread adds those up.
 template <bool WIDE, int K> struct GroupSum {
-    float (*buf)[K][32];
+    float (*buf)[K][16];
     int turn = 0;
     __device__ __forceinline__ void operator()(float (&v)[K], int G) {
 #pragma unroll
@@ -90,7 +96,7 @@ template <bool WIDE, int K> struct GroupSum {
         }
         if constexpr (WIDE) {
             const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = G >> 5;
-            float (&b)[K][32] = buf[turn];
+            float (&b)[K][16] = buf[turn];
             turn ^= 1;
             if (lane == 0) {
 #pragma unroll
@@ -99,72 +105,117 @@ template <bool WIDE, int K> struct GroupSum {
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                v[k] = lane < warps ? b[k][lane] : 0.0f;
+                v[k] = 0.0f;
 #pragma unroll
-                for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+                for (int w = 0; w < 16; w += 4)
+                    if (w < warps) {   // the places behind the last warp hold zeros
+                        const float4 f = *(const float4 *)&b[k][w];
+                        v[k] += (f.x + f.y) + (f.z + f.w);
+                    }
             }
         }
     }
 };
 
-// Rows of at most G V VE elements.  Thread t of a group holds the vectors t, t + G, ... of its row.
-template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a) {
-    __shared__ float red[2][1][32];
-    dependency_wait();
-    const int G = a.G, t = WIDE ? threadIdx.x : threadIdx.x & (G - 1);
-    const long long group = WIDE ? blockIdx.x : ((long long)blockIdx.x * blockDim.x + threadIdx.x) / G;
-    const long long groups = WIDE ? gridDim.x : (long long)gridDim.x * blockDim.x / G;
-    GroupSum<WIDE, 1> sum{red};
+// A thread's share of a row as pairs: element e of vector v is half e & 1 of pair (v VE + e) / 2.  Vectors behind the row's end hold zeros and
+// `in` is false for them; single values (VE == 1) share pairs two by two.  All arithmetic is on pairs: with one operation a value
+// the kernels were bound by issuing instructions (22 a value forward, 37 backward, 60 to 75 % of all slots), not by memory.
+template <int VE, int V> struct Share {
+    static constexpr int PAIRS = VE * V / 2;
     bool in[V];
-    float w[V][VE], b[V][VE];
+    __device__ __forceinline__ bool pair_in(int i) const { return VE == 1 ? in[2 * i] : in[2 * i / VE]; }
+    // a pair with zeros in the place of what is behind the row's end (only single values can be half in)
+    __device__ __forceinline__ f32x2 masked(int i, f32x2 x) const {
+        if constexpr (VE == 1) return make_float2(in[2 * i] ? x.x : 0.0f, in[2 * i + 1] ? x.y : 0.0f);
+        else return x;
+    }
+};
+template <typename IO, int VE, int V> __device__ __forceinline__ void unpack_row(const Raw<IO, VE> (&raw)[V], f32x2 (&f)[VE * V / 2]) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int c = (t + v * G) * VE;
-        in[v] = c < a.N;
+        float t[VE];
+        unpack<IO, VE>(raw[v], t);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) { w[v][e] = 1.0f; b[v][e] = 0.0f; }
-        if (in[v] && a.weight) load_f32<VE>(a.weight + c, w[v]);
-        if (in[v] && a.bias) load_f32<VE>(a.bias + c, b[v]);
+        for (int e = 0; e < VE; ++e) (v * VE + e & 1 ? f[(v * VE + e) / 2].y : f[(v * VE + e) / 2].x) = t[e];
     }
+}
+template <int VE, int V> __device__ __forceinline__ void load_vectors(const float *p, const bool (&in)[V], int G, float otherwise, f32x2 (&f)[VE * V / 2]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float t[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) t[e] = otherwise;
+        if (p && in[v]) load_f32<VE>(p + v * G * VE, t);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) (v * VE + e & 1 ? f[(v * VE + e) / 2].y : f[(v * VE + e) / 2].x) = t[e];
+    }
+}
+template <typename T, int VE, int V> __device__ __forceinline__ void store_vectors(T *p, const bool (&in)[V], int G, const f32x2 (&f)[VE * V / 2]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if (!in[v]) continue;
+        float t[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) t[e] = v * VE + e & 1 ? f[(v * VE + e) / 2].y : f[(v * VE + e) / 2].x;
+        store_vec<T, VE>(p + v * G * VE, t);
+    }
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { return fma2(a, pack2(1.0f, 1.0f), b); }
+__device__ __forceinline__ f32x2 both(float x) { return pack2(x, x); }
+
+// Rows of at most G V VE elements.  Thread t of a group holds the vectors t, t + G, ... of its row, the weights of its columns, and its next
+// row's vectors on their way.
+template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a) {
+    __shared__ float red[2][1][16];
+    constexpr int PAIRS = VE * V / 2;
+    if (WIDE && threadIdx.x < 32) red[threadIdx.x >> 4][0][threadIdx.x & 15] = 0.0f;
+    dependency_wait();
+    if (WIDE) __syncthreads();
+    const int G = a.G, t = WIDE ? threadIdx.x : threadIdx.x & (G - 1);
+    const long long groups = WIDE ? gridDim.x : (long long)gridDim.x * blockDim.x / G;
+    GroupSum<WIDE, 1> sum{red};
+    long long row = WIDE ? blockIdx.x : ((long long)blockIdx.x * blockDim.x + threadIdx.x) / G;
+    Share<VE, V> mine;
+#pragma unroll
+    for (int v = 0; v < V; ++v) mine.in[v] = (t + v * G) * VE < a.N;
+    f32x2 w[PAIRS], b[PAIRS];
+    load_vectors<VE, V>(a.weight ? a.weight + t * VE : nullptr, mine.in, G, 1.0f, w);
+    load_vectors<VE, V>(a.bias ? a.bias + t * VE : nullptr, mine.in, G, 0.0f, b);
     Raw<IO, VE> next[V] = {};
-    auto fetch = [&](long long row) {
-        const IO *p = (const IO *)a.x + row * a.N + t * VE;
+    auto fetch = [&](long long from) {
+        const IO *px = (const IO *)a.x + from * a.N + t * VE;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (in[v]) next[v] = load_raw<IO, VE>(p + v * G * VE);
+            if (mine.in[v]) next[v] = load_raw<IO, VE>(px + v * G * VE);
     };
-    if (group < a.rows) fetch(group);
+    if (row < a.rows) fetch(row);
     // all lanes of a warp stay in the loop while one of its groups has a row, for the shuffles; a wide group's block leaves as one
-    for (long long row = group; WIDE ? row < a.rows : __any_sync(0xffffffffu, row < a.rows); row += groups) {
-        float f[V][VE];
-#pragma unroll
-        for (int v = 0; v < V; ++v) unpack<IO, VE>(next[v], f[v]);
+    for (; WIDE ? row < a.rows : __any_sync(0xffffffffu, row < a.rows); row += groups) {
+        f32x2 f[PAIRS];
+        unpack_row<IO, VE, V>(next, f);
         if (row + groups < a.rows) fetch(row + groups);
         float s[1] = {0.0f};
+        f32x2 s2 = both(0.0f);
         if (a.center) {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int e = 0; e < VE; ++e) s[0] += in[v] ? f[v][e] : 0.0f;
+            for (int i = 0; i < PAIRS; ++i) s2 = add2(f[i], s2);
+            s[0] = s2.x + s2.y;
             sum(s, G);
         }
         const float mu = s[0] * a.inv_n;
-        s[0] = 0.0f;
+        s2 = both(0.0f);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) { f[v][e] -= mu; s[0] += in[v] ? f[v][e] * f[v][e] : 0.0f; }
+        for (int i = 0; i < PAIRS; ++i) {
+            f[i] = add2(f[i], both(-mu));
+            if (mine.pair_in(i)) { const f32x2 d = mine.masked(i, f[i]); s2 = fma2(d, d, s2); }
+        }
+        s[0] = s2.x + s2.y;
         sum(s, G);
         const float r = 1.0f / sqrtf(s[0] * a.inv_n + a.eps);
         if (row < a.rows) {
-            IO *p = (IO *)a.out + row * a.N + t * VE;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (!in[v]) continue;
-#pragma unroll
-                for (int e = 0; e < VE; ++e) f[v][e] = fmaf(f[v][e] * r, w[v][e], b[v][e]);
-                store_vec<IO, VE>(p + v * G * VE, f[v]);
-            }
+            for (int i = 0; i < PAIRS; ++i) f[i] = fma2(mul2(f[i], both(r)), w[i], b[i]);
+            store_vectors<IO, VE, V>((IO *)a.out + row * a.N + t * VE, mine.in, G, f);
             if (t == 0) {
                 if (a.mean) a.mean[row] = mu;
                 if (a.rstd) a.rstd[row] = r;
@@ -176,104 +227,118 @@ template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __lau
 
 // The gradients, rows as above.  The column sums of a group's rows stay in registers and leave once, added over the block's groups.
 template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_backward_kernel(NormArgs a) {
-    __shared__ float red[2][2][32];
+    __shared__ float red[2][2][16];
     extern __shared__ float cols[];   // narrow rows: [2][N] sums of the block
+    constexpr int PAIRS = VE * V / 2;
+    if (WIDE && threadIdx.x < 32) { red[threadIdx.x >> 4][0][threadIdx.x & 15] = 0.0f; red[threadIdx.x >> 4][1][threadIdx.x & 15] = 0.0f; }
     dependency_wait();
+    if (WIDE) __syncthreads();
     const int G = a.G, t = WIDE ? threadIdx.x : threadIdx.x & (G - 1);
     const long long group = WIDE ? blockIdx.x : ((long long)blockIdx.x * blockDim.x + threadIdx.x) / G;
     const long long groups = WIDE ? gridDim.x : (long long)gridDim.x * blockDim.x / G;
     GroupSum<WIDE, 2> sum{red};
-    bool in[V];
-    float w[V][VE], dw[V][VE] = {}, db[V][VE] = {};
+    Share<VE, V> mine;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int c = (t + v * G) * VE;
-        in[v] = c < a.N;
+    for (int v = 0; v < V; ++v) mine.in[v] = (t + v * G) * VE < a.N;
+    f32x2 w[PAIRS], dw[PAIRS], db[PAIRS];
+    load_vectors<VE, V>(a.weight ? a.weight + t * VE : nullptr, mine.in, G, 1.0f, w);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) w[v][e] = 1.0f;
-        if (in[v] && a.weight) load_f32<VE>(a.weight + c, w[v]);
-    }
+    for (int i = 0; i < PAIRS; ++i) dw[i] = db[i] = both(0.0f);
     Raw<IO, VE> nx[V] = {}, ny[V] = {};
     float nmu = 0.0f, nr = 0.0f;
     auto fetch = [&](long long row) {
         const IO *px = (const IO *)a.x + row * a.N + t * VE, *py = (const IO *)a.dy + row * a.N + t * VE;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (in[v]) { nx[v] = load_raw<IO, VE>(px + v * G * VE); ny[v] = load_raw<IO, VE>(py + v * G * VE); }
+            if (mine.in[v]) { nx[v] = load_raw<IO, VE>(px + v * G * VE); ny[v] = load_raw<IO, VE>(py + v * G * VE); }
         nmu = a.center ? a.mean_in[row] : 0.0f;
         nr = a.rstd_in[row];
     };
     if (group < a.rows) fetch(group);
     for (long long row = group; WIDE ? row < a.rows : __any_sync(0xffffffffu, row < a.rows); row += groups) {
         const bool live = row < a.rows;
-        float h[V][VE], g[V][VE];
+        f32x2 h[PAIRS], g[PAIRS];
         const float mu = nmu, r = nr;
-        float s[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            unpack<IO, VE>(nx[v], h[v]);
-            unpack<IO, VE>(ny[v], g[v]);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                h[v][e] = (h[v][e] - mu) * r;
-                if (live && in[v]) {
-                    dw[v][e] = fmaf(g[v][e], h[v][e], dw[v][e]);
-                    db[v][e] += g[v][e];
-                }
-                g[v][e] *= w[v][e];
-                if (in[v]) { s[0] = fmaf(g[v][e], h[v][e], s[0]); s[1] += g[v][e]; }
-            }
-        }
+        unpack_row<IO, VE, V>(nx, h);
+        unpack_row<IO, VE, V>(ny, g);   // zeros behind the row's end, so nothing of those columns counts in any sum
         if (row + groups < a.rows) fetch(row + groups);
+        f32x2 s0 = both(0.0f), s1 = both(0.0f);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            h[i] = mul2(add2(h[i], both(-mu)), both(r));
+            if (live) {
+                dw[i] = fma2(g[i], h[i], dw[i]);
+                db[i] = add2(g[i], db[i]);
+            }
+            g[i] = mul2(g[i], w[i]);
+            s0 = fma2(g[i], h[i], s0);
+            s1 = add2(g[i], s1);
+        }
+        float s[2] = {s0.x + s0.y, s1.x + s1.y};
         sum(s, G);
         const float c2 = s[0] * a.inv_n, c1 = a.center ? s[1] * a.inv_n : 0.0f;
         if (live) {
-            IO *p = (IO *)a.out + row * a.N + t * VE;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (!in[v]) continue;
-#pragma unroll
-                for (int e = 0; e < VE; ++e) g[v][e] = r * (fmaf(-h[v][e], c2, g[v][e]) - c1);
-                store_vec<IO, VE>(p + v * G * VE, g[v]);
-            }
+            for (int i = 0; i < PAIRS; ++i) g[i] = mul2(add2(fma2(h[i], both(-c2), g[i]), both(-c1)), both(r));
+            store_vectors<IO, VE, V>((IO *)a.out + row * a.N + t * VE, mine.in, G, g);
         }
     }
     dependency_trigger();
     if (a.part == nullptr) return;
     float *part = a.part + (size_t)blockIdx.x * 2 * a.N;
     if constexpr (WIDE) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (in[v])
-#pragma unroll
-                for (int e = 0; e < VE; ++e) { part[(t + v * G) * VE + e] = dw[v][e]; part[a.N + (t + v * G) * VE + e] = db[v][e]; }
+        store_vectors<float, VE, V>(part + t * VE, mine.in, G, dw);
+        store_vectors<float, VE, V>(part + a.N + t * VE, mine.in, G, db);
     } else {
         // the groups of a warp by shuffles, the warps of a block one after the other, in a fixed order
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int e = 0; e < VE; ++e)
-                for (int o = G; o < 32; o <<= 1) {
-                    dw[v][e] += __shfl_xor_sync(0xffffffffu, dw[v][e], o);
-                    db[v][e] += __shfl_xor_sync(0xffffffffu, db[v][e], o);
-                }
+        for (int i = 0; i < PAIRS; ++i)
+            for (int o = G; o < 32; o <<= 1) {
+                dw[i].x += __shfl_xor_sync(0xffffffffu, dw[i].x, o); dw[i].y += __shfl_xor_sync(0xffffffffu, dw[i].y, o);
+                db[i].x += __shfl_xor_sync(0xffffffffu, db[i].x, o); db[i].y += __shfl_xor_sync(0xffffffffu, db[i].y, o);
+            }
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
         for (int k = 0; k < warps; ++k) {
             if (warp == k && lane < G) {
 #pragma unroll
                 for (int v = 0; v < V; ++v)
-                    if (in[v])
+                    if (mine.in[v])
 #pragma unroll
                         for (int e = 0; e < VE; ++e) {
-                            const int c = (t + v * G) * VE + e;
+                            const int c = (t + v * G) * VE + e, i = v * VE + e;
+                            const float x = i & 1 ? dw[i / 2].y : dw[i / 2].x, y = i & 1 ? db[i / 2].y : db[i / 2].x;
                             const float p0 = k ? cols[c] : 0.0f, p1 = k ? cols[a.N + c] : 0.0f;
-                            if (k < warps - 1) { cols[c] = p0 + dw[v][e]; cols[a.N + c] = p1 + db[v][e]; }
-                            else { part[c] = p0 + dw[v][e]; part[a.N + c] = p1 + db[v][e]; }
+                            if (k < warps - 1) { cols[c] = p0 + x; cols[a.N + c] = p1 + y; }
+                            else { part[c] = p0 + x; part[a.N + c] = p1 + y; }
                         }
             }
             __syncthreads();
         }
     }
+}
+
+// dweight | dbias = the sums of the blocks' columns: a block of 32 warps for 32 columns, every warp a 32nd of the parts, added up in a fixed order
+__global__ void __launch_bounds__(1024) norm_columns_kernel(const float *part, int parts, int N, float *dweight, float *dbias) {
+    __shared__ float red[32][33];
+    dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long c = (long long)blockIdx.x * 32 + lane, stride = 2ll * N;
+    float s = 0.0f;
+    if (c < stride) {
+#pragma unroll 8
+        for (int p = warp; p < parts; p += 32) s += part[p * stride + c];
+    }
+    red[warp][lane] = s;
+    __syncthreads();
+    s = red[lane][warp];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const long long col = (long long)blockIdx.x * 32 + warp;
+    if (lane == 0 && col < stride) {
+        float *const out = col < N ? dweight : dbias;
+        if (out) out[col < N ? col : col - N] = s;
+    }
+    dependency_trigger();
 }
 
 // Rows that no block holds in registers: a block reads its row three times (the second and third time mostly out of L2).
@@ -285,23 +350,23 @@ template <typename IO> __device__ __forceinline__ void put(void *p, long long i,
     const float f[1] = {v};
     store_vec<IO, 1>((IO *)p + i, f);
 }
-template <typename IO> __global__ void __launch_bounds__(1024) norm_long_kernel(NormArgs a) {
-    __shared__ float red[2][1][32];
+template <typename IO> __global__ void __launch_bounds__(512) norm_long_kernel(NormArgs a) {
+    __shared__ float red[2][1][16];
     dependency_wait();
     GroupSum<true, 1> sum{red};
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const long long base = row * a.N;
         float s[1] = {0.0f};
         if (a.center) {
-            for (int c = threadIdx.x; c < a.N; c += 1024) s[0] += at<IO>(a.x, base + c);
-            sum(s, 1024);
+            for (int c = threadIdx.x; c < a.N; c += 512) s[0] += at<IO>(a.x, base + c);
+            sum(s, 512);
         }
         const float mu = s[0] * a.inv_n;
         s[0] = 0.0f;
-        for (int c = threadIdx.x; c < a.N; c += 1024) { const float d = at<IO>(a.x, base + c) - mu; s[0] = fmaf(d, d, s[0]); }
-        sum(s, 1024);
+        for (int c = threadIdx.x; c < a.N; c += 512) { const float d = at<IO>(a.x, base + c) - mu; s[0] = fmaf(d, d, s[0]); }
+        sum(s, 512);
         const float r = 1.0f / sqrtf(s[0] * a.inv_n + a.eps);
-        for (int c = threadIdx.x; c < a.N; c += 1024)
+        for (int c = threadIdx.x; c < a.N; c += 512)
             put<IO>(a.out, base + c, fmaf((at<IO>(a.x, base + c) - mu) * r, a.weight ? a.weight[c] : 1.0f, a.bias ? a.bias[c] : 0.0f));
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mu;
@@ -310,22 +375,22 @@ template <typename IO> __global__ void __launch_bounds__(1024) norm_long_kernel(
     }
     dependency_trigger();
 }
-template <typename IO> __global__ void __launch_bounds__(1024) norm_long_backward_kernel(NormArgs a) {
-    __shared__ float red[2][2][32];
+template <typename IO> __global__ void __launch_bounds__(512) norm_long_backward_kernel(NormArgs a) {
+    __shared__ float red[2][2][16];
     dependency_wait();
     GroupSum<true, 2> sum{red};
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const long long base = row * a.N;
         const float mu = a.center ? a.mean_in[row] : 0.0f, r = a.rstd_in[row];
         float s[2] = {0.0f, 0.0f};
-        for (int c = threadIdx.x; c < a.N; c += 1024) {
+        for (int c = threadIdx.x; c < a.N; c += 512) {
             const float g = at<IO>(a.dy, base + c) * (a.weight ? a.weight[c] : 1.0f);
             s[0] = fmaf(g, (at<IO>(a.x, base + c) - mu) * r, s[0]);
             s[1] += g;
         }
-        sum(s, 1024);
+        sum(s, 512);
         const float c2 = s[0] * a.inv_n, c1 = a.center ? s[1] * a.inv_n : 0.0f;
-        for (int c = threadIdx.x; c < a.N; c += 1024) {
+        for (int c = threadIdx.x; c < a.N; c += 512) {
             const float g = at<IO>(a.dy, base + c) * (a.weight ? a.weight[c] : 1.0f);
             put<IO>(a.out, base + c, r * (fmaf(-(at<IO>(a.x, base + c) - mu) * r, c2, g) - c1));
         }
@@ -352,21 +417,15 @@ template <typename IO> __global__ void __launch_bounds__(256) norm_long_columns_
 // How a row is laid out over threads: elements a load (VE), loads a thread (V), threads (G); V == 0: the long kernels
 struct Layout { int VE, V, G; bool wide; };
 Layout norm_layout(int N, int io, bool backward) {
-    const int ve = io == RGLRU_BF16 ? 8 : 4;
-    if (N % ve == 0) {   // 16-byte accesses: every row starts on a 16-byte boundary
-        const int n = N / ve;
-        if (n <= 8) return {ve, 1, 8, false};
-        if (n <= 16) return {ve, 2, 8, false};
-        if (n <= 32) return {ve, 2, 16, false};
-        if (n <= 64) return {ve, 2, 32, false};
-        if (n <= (backward ? 1024 : 2048)) return {ve, 2, ceil_div((size_t)n, 64) * 32, true};   // the backward's column sums fit 512 threads' registers
-        return {ve, 0, 1024, true};
-    }
-    if (N <= 64) return {1, 8, 8, false};
-    if (N <= 128) return {1, 8, 16, false};
-    if (N <= 256) return {1, 8, 32, false};
-    if (N <= 8192) return {1, 8, ceil_div((size_t)N, 256) * 32, true};
-    return {1, 0, 1024, true};
+    int ve = io == RGLRU_BF16 ? 8 : 4;
+    const int most = ve;
+    while (N % ve) ve /= 2;   // every row starts at a multiple of the access
+    const int n = N / ve;
+    const int v = ve == most ? (n > 128 && !backward ? 4 : 2) : ve == 1 || ve * 4 == most ? 8 : 4;
+    for (int g = 4; g <= 32; g *= 2)
+        if (n <= g * v) return {ve, v, g, false};
+    if (n <= v * 512) return {ve, v, ceil_div((size_t)n, 32 * v) * 32, true};
+    return {ve, 0, 512, true};
 }
 
 constexpr int NORM_SMS = 148;   // the block count is part of the workspace's size, so it does not depend on the device
@@ -376,34 +435,36 @@ int backward_blocks(const rglru_norm_shape_t *s, const Layout &l) {
     if (l.V == 0) return (int)(s->rows < LONG_COLUMN_SPLITS ? s->rows : LONG_COLUMN_SPLITS);
     const int threads = l.wide ? l.G : 256;
     const long long need = l.wide ? s->rows : (s->rows + 256 / l.G - 1) / (256 / l.G);
-    const int per_sm = threads >= 1024 ? 1 : 1024 / threads;
-    const long long most = (long long)NORM_SMS * per_sm;
+    const long long most = (long long)NORM_SMS * (threads > 256 ? 1 : 512 / threads);
     return (int)(need < most ? need : most);
 }
 
-template <typename IO, int VE> cudaError_t launch_norm(const Layout &l, bool backward, unsigned blocks, const NormArgs &a, cudaStream_t st) {
-    const dim3 grid(blocks), block(l.wide ? l.G : 256);
-    const size_t smem = backward && !l.wide ? (size_t)2 * a.N * sizeof(float) : 0;
-#define RGLRU_NORM(V, WIDE, MAXT)                                                                       \
-    return backward ? launch_dependent(norm_backward_kernel<IO, VE, V, WIDE, MAXT>, grid, block, smem, st, a) \
-                    : launch_dependent(norm_kernel<IO, VE, V, WIDE, MAXT>, grid, block, 0, st, a)
-    if constexpr (VE == 1) {
-        if (l.G > 512) { RGLRU_NORM(8, true, 1024); }
-        if (l.wide) { RGLRU_NORM(8, true, 512); }
-        RGLRU_NORM(8, false, 256);
-    } else {
-        if (l.G > 512) return launch_dependent(norm_kernel<IO, VE, 2, true, 1024>, grid, block, 0, st, a);   // forward only
-        if (l.wide) { RGLRU_NORM(2, true, 512); }
-        if (l.V == 1) { RGLRU_NORM(1, false, 256); }
-        RGLRU_NORM(2, false, 256);
-    }
-#undef RGLRU_NORM
+template <typename IO, int VE, int V> cudaError_t launch_forward(const Layout &l, unsigned blocks, const NormArgs &a, cudaStream_t st) {
+    return l.wide ? launch_dependent(norm_kernel<IO, VE, V, true, 512>, dim3(blocks), dim3(l.G), 0, st, a)
+                  : launch_dependent(norm_kernel<IO, VE, V, false, 256>, dim3(blocks), dim3(256), 0, st, a);
+}
+template <typename IO, int VE, int V> cudaError_t launch_backward(const Layout &l, unsigned blocks, const NormArgs &a, cudaStream_t st) {
+    return l.wide ? launch_dependent(norm_backward_kernel<IO, VE, V, true, 512>, dim3(blocks), dim3(l.G), 0, st, a)
+                  : launch_dependent(norm_backward_kernel<IO, VE, V, false, 256>, dim3(blocks), dim3(256), (size_t)2 * a.N * sizeof(float), st, a);
 }
 template <typename IO> cudaError_t launch_norm(const Layout &l, bool backward, unsigned blocks, const NormArgs &a, cudaStream_t st) {
+    constexpr int MOST = 16 / sizeof(IO);
     if (l.V == 0)
-        return backward ? launch_dependent(norm_long_backward_kernel<IO>, dim3(blocks), dim3(1024), 0, st, a)
-                        : launch_dependent(norm_long_kernel<IO>, dim3(blocks), dim3(1024), 0, st, a);
-    return l.VE == 1 ? launch_norm<IO, 1>(l, backward, blocks, a, st) : launch_norm<IO, 16 / sizeof(IO)>(l, backward, blocks, a, st);
+        return backward ? launch_dependent(norm_long_backward_kernel<IO>, dim3(blocks), dim3(512), 0, st, a)
+                        : launch_dependent(norm_long_kernel<IO>, dim3(blocks), dim3(512), 0, st, a);
+#define RGLRU_NORM(VE, V) return backward ? launch_backward<IO, VE, V>(l, blocks, a, st) : launch_forward<IO, VE, V>(l, blocks, a, st)
+    if (l.VE == MOST) {
+        if (l.V == 4) return launch_forward<IO, MOST, 4>(l, blocks, a, st);
+        RGLRU_NORM(MOST, 2);
+    }
+    if constexpr (MOST == 8) {
+        if (l.VE == 4) { RGLRU_NORM(4, 4); }
+        if (l.VE == 2) { RGLRU_NORM(2, 8); }
+    } else {
+        if (l.VE == 2) { RGLRU_NORM(2, 4); }
+    }
+    RGLRU_NORM(1, 8);
+#undef RGLRU_NORM
 }
 
 int32_t check_norm(const rglru_norm_shape_t *s) {
@@ -436,8 +497,7 @@ int32_t rglru_layer_norm(const rglru_norm_shape_t *s, const void *x, const float
     const Layout l = norm_layout(s->N, s->io, false);
     NormArgs a = norm_args(s, l);
     a.x = x; a.weight = weight; a.bias = bias; a.out = y; a.mean = mean; a.rstd = rstd;
-    const int threads = l.wide ? l.G : 256;
-    const long long need = l.wide ? s->rows : (s->rows + 256 / l.G - 1) / (256 / l.G), most = (long long)num_sms() * (2048 / threads);
+    const long long need = l.wide ? s->rows : (s->rows + 256 / l.G - 1) / (256 / l.G), threads = l.wide ? l.G : 256, most = (long long)num_sms() * (threads > 256 ? 2 : 1024 / threads);
     const unsigned blocks = (unsigned)(need < most ? need : most);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     return call_status(s->io == RGLRU_F32 ? launch_norm<float>(l, false, blocks, a, st) : launch_norm<__nv_bfloat16>(l, false, blocks, a, st));
@@ -471,11 +531,8 @@ int32_t rglru_layer_norm_backward(const rglru_norm_shape_t *s, const void *dy, c
     cudaError_t e = f32 ? launch_norm<float>(l, true, grid, a, st) : launch_norm<__nv_bfloat16>(l, true, grid, a, st);
     if (e == cudaSuccess && sums && l.V == 0)
         e = launch_dependent(f32 ? norm_long_columns_kernel<float> : norm_long_columns_kernel<__nv_bfloat16>, dim3((s->N + 255) / 256, blocks), dim3(256), 0, st, a);
-    if (e == cudaSuccess && sums) {
-        ReduceJobs jobs{};
-        add_reduce_job(jobs, a.part, blocks, (size_t)2 * s->N, dweight, s->N, dbias, s->N, nullptr, 0);
-        e = run_reduce_jobs(jobs, st);
-    }
+    if (e == cudaSuccess && sums)
+        e = launch_dependent(norm_columns_kernel, dim3((unsigned)((2ll * s->N + 31) / 32)), dim3(1024), 0, st, (const float *)a.part, blocks, (int)s->N, dweight, dbias);
     return call_status(e);
 }
 
