@@ -225,6 +225,17 @@ template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __lau
     dependency_trigger();
 }
 
+// 16-byte copies into a part of shared memory that is the thread's own
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ uint4 own16(uint32_t src) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(src) : "memory");
+    return v;
+}
+constexpr int AHEAD = 3;   // rows that a wide row's threads have on their way in shared memory (one in registers: 16384 x 4096 bf16 83 us instead of 72)
+
 // The gradients, rows as above.  The column sums of a group's rows stay in registers and leave once, added over the block's groups.
 template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_backward_kernel(NormArgs a) {
     __shared__ float red[2][2][16];
@@ -244,24 +255,49 @@ template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __lau
     load_vectors<VE, V>(a.weight ? a.weight + t * VE : nullptr, mine.in, G, 1.0f, w);
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) dw[i] = db[i] = both(0.0f);
+    constexpr bool RING = WIDE && VE * sizeof(IO) == 16;
     Raw<IO, VE> nx[V] = {}, ny[V] = {};
     float nmu = 0.0f, nr = 0.0f;
-    auto fetch = [&](long long row) {
+    const uint32_t own = smem_u32(cols) + threadIdx.x * 16, row_bytes = blockDim.x * 16;
+    auto fetch = [&](int slot, long long row) {
         const IO *px = (const IO *)a.x + row * a.N + t * VE, *py = (const IO *)a.dy + row * a.N + t * VE;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (mine.in[v]) { nx[v] = load_raw<IO, VE>(px + v * G * VE); ny[v] = load_raw<IO, VE>(py + v * G * VE); }
+        for (int v = 0; v < V; ++v) {
+            if (!mine.in[v] || row >= a.rows) continue;
+            if constexpr (RING) {
+                copy16(own + (slot * 2 * V + v) * row_bytes, px + v * G * VE);
+                copy16(own + (slot * 2 * V + V + v) * row_bytes, py + v * G * VE);
+            } else {
+                nx[v] = load_raw<IO, VE>(px + v * G * VE);
+                ny[v] = load_raw<IO, VE>(py + v * G * VE);
+            }
+        }
+        if (RING) copies_begun();
+    };
+    auto fetch_statistics = [&](long long row) {
+        if (row >= a.rows) return;
         nmu = a.center ? a.mean_in[row] : 0.0f;
         nr = a.rstd_in[row];
     };
-    if (group < a.rows) fetch(group);
+#pragma unroll
+    for (int k = 0; k < (RING ? AHEAD : 1); ++k) fetch(k, group + k * groups);
+    fetch_statistics(group);
+    int slot = 0;
     for (long long row = group; WIDE ? row < a.rows : __any_sync(0xffffffffu, row < a.rows); row += groups) {
         const bool live = row < a.rows;
         f32x2 h[PAIRS], g[PAIRS];
         const float mu = nmu, r = nr;
+        if constexpr (RING) {
+            copies_wait<AHEAD - 1>();
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (mine.in[v]) { nx[v] = own16(own + (slot * 2 * V + v) * row_bytes); ny[v] = own16(own + (slot * 2 * V + V + v) * row_bytes); }
+        }
         unpack_row<IO, VE, V>(nx, h);
         unpack_row<IO, VE, V>(ny, g);   // zeros behind the row's end, so nothing of those columns counts in any sum
-        if (row + groups < a.rows) fetch(row + groups);
+        fetch(slot, row + (RING ? AHEAD : 1) * groups);
+        slot = slot + 1 == AHEAD ? 0 : slot + 1;
+        fetch_statistics(row + groups);
         f32x2 s0 = both(0.0f), s1 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) {
@@ -433,28 +469,47 @@ constexpr int LONG_COLUMN_SPLITS = 32;
 // Blocks of the backward: a block's column sums are 2 N floats of extra traffic each way
 int backward_blocks(const rglru_norm_shape_t *s, const Layout &l) {
     if (l.V == 0) return (int)(s->rows < LONG_COLUMN_SPLITS ? s->rows : LONG_COLUMN_SPLITS);
-    const int threads = l.wide ? l.G : 256;
+    const int threads = l.wide ? l.G : 256, most_threads = s->io == RGLRU_F32 ? 1024 : 512, resident = threads > most_threads / 2 ? 1 : most_threads / threads;
     const long long need = l.wide ? s->rows : (s->rows + 256 / l.G - 1) / (256 / l.G);
-    const long long most = (long long)NORM_SMS * (threads > 256 ? 1 : 512 / threads);
+    const long long most = (long long)NORM_SMS * resident;
     return (int)(need < most ? need : most);
 }
 
-template <typename IO, int VE, int V> cudaError_t launch_forward(const Layout &l, unsigned blocks, const NormArgs &a, cudaStream_t st) {
-    return l.wide ? launch_dependent(norm_kernel<IO, VE, V, true, 512>, dim3(blocks), dim3(l.G), 0, st, a)
-                  : launch_dependent(norm_kernel<IO, VE, V, false, 256>, dim3(blocks), dim3(256), 0, st, a);
+// Blocks walk rows, so there are as many as are resident at a time: more would run in a second round beside idle SMs
+template <typename K> cudaError_t launch_resident(K kernel, long long need, int threads, const NormArgs &a, cudaStream_t st) {
+    const int sms = num_sms();
+    int per_sm = 1;
+    if (need > sms) {
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0);
+        if (e != cudaSuccess) return e;
+        if (per_sm < 1) per_sm = 1;
+    }
+    const long long most = (long long)sms * per_sm;
+    return launch_dependent(kernel, dim3((unsigned)(need < most ? need : most)), dim3(threads), 0, st, a);
+}
+template <typename IO, int VE, int V> cudaError_t launch_forward(const Layout &l, const NormArgs &a, cudaStream_t st) {
+    return l.wide ? launch_resident(norm_kernel<IO, VE, V, true, 512>, a.rows, l.G, a, st)
+                  : launch_resident(norm_kernel<IO, VE, V, false, 256>, (a.rows + 256 / l.G - 1) / (256 / l.G), 256, a, st);
 }
 template <typename IO, int VE, int V> cudaError_t launch_backward(const Layout &l, unsigned blocks, const NormArgs &a, cudaStream_t st) {
-    return l.wide ? launch_dependent(norm_backward_kernel<IO, VE, V, true, 512>, dim3(blocks), dim3(l.G), 0, st, a)
-                  : launch_dependent(norm_backward_kernel<IO, VE, V, false, 256>, dim3(blocks), dim3(256), (size_t)2 * a.N * sizeof(float), st, a);
+    if (!l.wide) return launch_dependent(norm_backward_kernel<IO, VE, V, false, 256>, dim3(blocks), dim3(256), (size_t)2 * a.N * sizeof(float), st, a);
+    size_t smem = 0;
+    if constexpr (VE * sizeof(IO) == 16) {
+        static PerDeviceOptIn opt;
+        const cudaError_t e = opt.ensure(norm_backward_kernel<IO, VE, V, true, 512>, AHEAD * 2 * V * 16 * 512);
+        if (e != cudaSuccess) return e;
+        smem = (size_t)AHEAD * 2 * V * 16 * l.G;
+    }
+    return launch_dependent(norm_backward_kernel<IO, VE, V, true, 512>, dim3(blocks), dim3(l.G), smem, st, a);
 }
 template <typename IO> cudaError_t launch_norm(const Layout &l, bool backward, unsigned blocks, const NormArgs &a, cudaStream_t st) {
     constexpr int MOST = 16 / sizeof(IO);
     if (l.V == 0)
         return backward ? launch_dependent(norm_long_backward_kernel<IO>, dim3(blocks), dim3(512), 0, st, a)
-                        : launch_dependent(norm_long_kernel<IO>, dim3(blocks), dim3(512), 0, st, a);
-#define RGLRU_NORM(VE, V) return backward ? launch_backward<IO, VE, V>(l, blocks, a, st) : launch_forward<IO, VE, V>(l, blocks, a, st)
+                        : launch_resident(norm_long_kernel<IO>, a.rows, 512, a, st);
+#define RGLRU_NORM(VE, V) return backward ? launch_backward<IO, VE, V>(l, blocks, a, st) : launch_forward<IO, VE, V>(l, a, st)
     if (l.VE == MOST) {
-        if (l.V == 4) return launch_forward<IO, MOST, 4>(l, blocks, a, st);
+        if (l.V == 4) return launch_forward<IO, MOST, 4>(l, a, st);
         RGLRU_NORM(MOST, 2);
     }
     if constexpr (MOST == 8) {
@@ -497,10 +552,8 @@ int32_t rglru_layer_norm(const rglru_norm_shape_t *s, const void *x, const float
     const Layout l = norm_layout(s->N, s->io, false);
     NormArgs a = norm_args(s, l);
     a.x = x; a.weight = weight; a.bias = bias; a.out = y; a.mean = mean; a.rstd = rstd;
-    const long long need = l.wide ? s->rows : (s->rows + 256 / l.G - 1) / (256 / l.G), threads = l.wide ? l.G : 256, most = (long long)num_sms() * (threads > 256 ? 2 : 1024 / threads);
-    const unsigned blocks = (unsigned)(need < most ? need : most);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    return call_status(s->io == RGLRU_F32 ? launch_norm<float>(l, false, blocks, a, st) : launch_norm<__nv_bfloat16>(l, false, blocks, a, st));
+    return call_status(s->io == RGLRU_F32 ? launch_norm<float>(l, false, 0, a, st) : launch_norm<__nv_bfloat16>(l, false, 0, a, st));
 }
 
 size_t rglru_layer_norm_workspace_bytes(const rglru_norm_shape_t *s) {
