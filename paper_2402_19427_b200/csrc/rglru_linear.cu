@@ -80,6 +80,64 @@ template <typename IO> __global__ void __launch_bounds__(256) generic_linear_ker
     dependency_trigger();
 }
 
+// The forward of few rows (tokens): bound by reading the weights once.  A warp takes two outputs; its lanes read 16 bytes of each weight row side by
+// side, and the same columns of up to MT rows of x out of the first-level cache.  Tensor cores would need the weights in shared memory
+// first, the tokens padded and K split over the SMs: 11.4 us for one token of 2560 x 2560.
+template <typename IO, int VE, int MT> __global__ void __launch_bounds__(256) few_rows_kernel(GenericGemm g) {
+    dependency_wait();
+    const int lane = threadIdx.x & 31;
+    const long long n0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * 2;
+    if (n0 < g.N) {
+        const IO *w0 = (const IO *)g.b + n0 * g.K, *w1 = n0 + 1 < g.N ? w0 + g.K : w0;
+        float acc[2][MT] = {};
+#pragma unroll 4
+        for (long long k = lane * VE; k < g.K; k += 32 * VE) {
+            float a[VE], b[VE];
+            LinearVec<IO, VE>::load(w0 + k, a);
+            LinearVec<IO, VE>::load(w1 + k, b);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                if (m >= g.M) break;
+                float x[VE];
+                LinearVec<IO, VE>::load((const IO *)g.a + m * g.K + k, x);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) { acc[0][m] = fmaf(a[e], x[e], acc[0][m]); acc[1][m] = fmaf(b[e], x[e], acc[1][m]); }
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                acc[0][m] += __shfl_xor_sync(0xffffffffu, acc[0][m], o);
+                acc[1][m] += __shfl_xor_sync(0xffffffffu, acc[1][m], o);
+            }
+        }
+        // lane (2 m + i) finishes output i of row m
+        float z = 0.0f;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) z = lane == 2 * m ? acc[0][m] : lane == 2 * m + 1 ? acc[1][m] : z;
+        const long long m = lane >> 1, n = n0 + (lane & 1);
+        if (m < g.M && m < MT && n < g.N) {
+            const LinearEpilogue &e = g.e;
+            const long long o = m * g.N + n;
+            z += e.bias ? e.bias[n] : 0.0f;
+            if (e.preact) put<IO>(e.preact, o, z);
+            put<IO>(e.y, o, activate<sizeof(IO) == 2>(z, e.activation) + (e.residual ? at<IO>(e.residual, o) : 0.0f));
+        }
+    }
+    dependency_trigger();
+}
+constexpr int FEW_ROWS = 8;
+template <typename IO, int VE> cudaError_t few_rows(const GenericGemm &g, cudaStream_t st) {
+    const dim3 grid((unsigned)((g.N + 15) / 16));
+    return launch_dependent(g.M == 1 ? few_rows_kernel<IO, VE, 1> : g.M == 2 ? few_rows_kernel<IO, VE, 2> : g.M <= 4 ? few_rows_kernel<IO, VE, 4> : few_rows_kernel<IO, VE, 8>,
+                            grid, dim3(256), 0, st, g);
+}
+template <typename IO> cudaError_t few_rows(const GenericGemm &g, cudaStream_t st) {
+    constexpr int MOST = 16 / sizeof(IO);
+    return g.K % MOST == 0 ? few_rows<IO, MOST>(g, st) : few_rows<IO, 1>(g, st);
+}
+
 // dz = dy act'(z) in the io type, and the sums of the unrounded dz over a block's rows.  A thread owns VE columns and walks rows.
 struct DzArgs {
     long long M;
@@ -105,8 +163,17 @@ template <typename IO, int VE> __global__ void __launch_bounds__(256) linear_dz_
             if (a.activation != RGLRU_ACT_NONE) {
                 float z[VE];
                 LinearVec<IO, VE>::load((const IO *)a.preact + o, z);
+                if constexpr (sizeof(IO) == 2 && VE > 1) {
 #pragma unroll
-                for (int e = 0; e < VE; ++e) g[e] *= activation_slope<sizeof(IO) == 2>(z[e], a.activation);
+                    for (int e = 0; e < VE; e += 2) {
+                        const float2 d = slope_fast(make_float2(z[e], z[e + 1]), a.activation);
+                        g[e] *= d.x;
+                        g[e + 1] *= d.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) g[e] *= activation_slope<sizeof(IO) == 2>(z[e], a.activation);
+                }
                 if (a.dz) LinearVec<IO, VE>::store((IO *)a.dz + o, g);
             }
 #pragma unroll
@@ -163,6 +230,7 @@ LinearProduct dw_product(const rglru_linear_shape_t *s, const void *dz, const vo
 }
 bool on_tensor_cores(const rglru_linear_shape_t *s, const LinearProduct &g) { return !(s->flags & RGLRU_FLAG_FORCE_GENERIC) && sm100_linear_wanted(g); }
 size_t product_bytes(const rglru_linear_shape_t *s, const LinearProduct &g) { return on_tensor_cores(s, g) ? sm100_linear_bytes(g) : 0; }
+bool is_few_rows(const rglru_linear_shape_t *s) { return !(s->flags & RGLRU_FLAG_FORCE_GENERIC) && s->M <= FEW_ROWS; }
 cudaError_t run_product(const rglru_linear_shape_t *s, const LinearProduct &g, void *scratch, void *workspace, cudaStream_t st) {
     if (on_tensor_cores(s, g)) return sm100_linear(g, scratch, (uint32_t *)workspace, st);
     auto by_row = [](const LinearOperand &o) { return o.turned ? 1ll : o.cols; };
@@ -187,6 +255,7 @@ extern "C" {
 
 size_t rglru_linear_workspace_bytes(const rglru_linear_shape_t *s, int32_t op) {
     if (check_linear(s) != RGLRU_OK || (op != RGLRU_OP_PREFILL && op != RGLRU_OP_BACKWARD)) return 0;
+    if (op == RGLRU_OP_PREFILL && is_few_rows(s)) return WS_HEADER_BYTES;
     if (op == RGLRU_OP_PREFILL) return WS_HEADER_BYTES + product_bytes(s, forward_product(s, nullptr, nullptr, {}));
     size_t bytes = WS_HEADER_BYTES + up256((size_t)dz_blocks(s) * s->N * sizeof(float));
     if (s->activation != RGLRU_ACT_NONE) bytes += up256((size_t)s->M * s->N * io_bytes(s->io));
@@ -208,6 +277,10 @@ int32_t rglru_linear(const rglru_linear_shape_t *s, const void *x, const void *w
         overlap(preact, yb, weight, wb) || overlap(preact, yb, residual, yb) || overlap(preact, yb, y, yb))
         return RGLRU_ERR_ALIAS;
     const LinearProduct g = forward_product(s, x, weight, {bias, residual, y, preact, s->activation});
+    if (is_few_rows(s)) {
+        const GenericGemm f{x, weight, s->K, 1, s->K, 1, s->M, s->N, s->K, g.e};
+        return call_status(s->io == RGLRU_F32 ? few_rows<float>(f, (cudaStream_t)cuda_stream) : few_rows<__nv_bfloat16>(f, (cudaStream_t)cuda_stream));
+    }
     return call_status(run_product(s, g, (char *)workspace + WS_HEADER_BYTES, workspace, (cudaStream_t)cuda_stream));
 }
 

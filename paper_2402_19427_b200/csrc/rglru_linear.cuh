@@ -38,44 +38,65 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
 // element-wise kernels and epilogues are bound by memory or the tensor cores again.  At the infinities GeLU and SiLU are 0 and
 // infinity, their slopes 0 and 1, where their formulas have 0 * inf.
 constexpr float SQRT_HALF = 0.70710678118654752440f, INV_SQRT_2PI = 0.39894228040143267794f, LOG2_E = 1.44269504088896340736f;
-struct Normal { float tail, density; };   // Phi(-|z|) and exp(-z^2 / 2), for |z| held at 30
-__device__ __forceinline__ Normal normal_tail(float z) {
-    const float a = fabsf(z) > 30.0f ? 30.0f : fabsf(z);   // NaN stays
-    const float t = ptx::rcp_approx(fmaf(a, 0.3275911f * SQRT_HALF, 1.0f));
-    float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-    p = fmaf(p, t, 0.5f * 1.421413741f); p = fmaf(p, t, 0.5f * -0.284496736f); p = fmaf(p, t, 0.5f * 0.254829592f);
-    const float e = ptx::ex2_approx(a * a * (-0.5f * LOG2_E));
-    return {p * t * e, e};
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) { return ptx::fma2(a, b, c); }
+__device__ __forceinline__ float2 both_of(float x) { return make_float2(x, x); }
+// Phi(-|z|) and exp(-z^2 / 2) of two values whose magnitudes a are held at 30
+struct Normal { float2 tail, density; };
+__device__ __forceinline__ Normal normal_tail(float2 a) {
+    const float2 d = fma_pair(a, both_of(0.3275911f * SQRT_HALF), both_of(1.0f));
+    const float2 t = make_float2(ptx::rcp_approx(d.x), ptx::rcp_approx(d.y));
+    float2 p = fma_pair(t, both_of(0.5f * 1.061405429f), both_of(0.5f * -1.453152027f));
+    p = fma_pair(p, t, both_of(0.5f * 1.421413741f));
+    p = fma_pair(p, t, both_of(0.5f * -0.284496736f));
+    p = fma_pair(p, t, both_of(0.5f * 0.254829592f));
+    const float2 x = ptx::mul2(ptx::mul2(a, a), both_of(-0.5f * LOG2_E));
+    const float2 e = make_float2(ptx::ex2_approx(x.x), ptx::ex2_approx(x.y));
+    return {ptx::mul2(ptx::mul2(p, t), e), e};
 }
-template <bool FAST> __device__ __forceinline__ float sigmoid_of(float z) {
-    if constexpr (FAST) return ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * z));
-    else return 1.0f / (1.0f + expf(-z));
+__device__ __forceinline__ float held(float z, float most) { return z > most ? most : z < -most ? -most : z; }   // NaN stays
+// for bf16 results
+__device__ __forceinline__ float2 activate_fast(float2 z, int kind) {
+    if (kind == RGLRU_ACT_NONE) return z;
+    if (kind == RGLRU_ACT_GELU) {
+        const float2 a = make_float2(fabsf(held(z.x, 30.0f)), fabsf(held(z.y, 30.0f)));
+        return fma_pair(make_float2(-a.x, -a.y), normal_tail(a).tail, make_float2(z.x > 0.0f ? z.x : 0.0f, z.y > 0.0f ? z.y : 0.0f));
+    }
+    const float2 s = make_float2(ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * z.x)), ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * z.y)));
+    return make_float2(z.x < -100.0f ? 0.0f : z.x * s.x, z.y < -100.0f ? 0.0f : z.y * s.y);
+}
+__device__ __forceinline__ float2 slope_fast(float2 z, int kind) {
+    if (kind == RGLRU_ACT_GELU) {
+        const float2 c = make_float2(held(z.x, 30.0f), held(z.y, 30.0f));
+        const Normal n = normal_tail(make_float2(fabsf(c.x), fabsf(c.y)));
+        const float2 phi = make_float2(c.x > 0.0f ? 1.0f - n.tail.x : n.tail.x, c.y > 0.0f ? 1.0f - n.tail.y : n.tail.y);
+        return fma_pair(ptx::mul2(c, both_of(INV_SQRT_2PI)), n.density, phi);
+    }
+    const float2 c = make_float2(held(z.x, 100.0f), held(z.y, 100.0f));
+    const float2 s = make_float2(ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * c.x)), ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * c.y)));
+    return ptx::mul2(s, fma_pair(c, make_float2(1.0f - s.x, 1.0f - s.y), both_of(1.0f)));
+}
+// for fp32 results; out of line, since the libraries' functions are long
+static __device__ __noinline__ float activate_exact(float z, int kind) {
+    if (kind == RGLRU_ACT_GELU) return z == -INFINITY ? 0.0f : z * (0.5f * erfcf(-z * SQRT_HALF));
+    return z < -100.0f ? 0.0f : z / (1.0f + expf(-z));
+}
+static __device__ __noinline__ float slope_exact(float z, int kind) {
+    if (kind == RGLRU_ACT_GELU) {
+        const float c = held(z, 30.0f);
+        return fmaf(c * INV_SQRT_2PI, expf(-0.5f * c * c), 0.5f * erfcf(-c * SQRT_HALF));
+    }
+    const float c = held(z, 100.0f), s = 1.0f / (1.0f + expf(-c));
+    return s * fmaf(c, 1.0f - s, 1.0f);
 }
 template <bool FAST> __device__ __forceinline__ float activate(float z, int kind) {
     if (kind == RGLRU_ACT_NONE) return z;
-    if (kind == RGLRU_ACT_GELU) {
-        if constexpr (FAST) {
-            const float a = fabsf(z) > 30.0f ? 30.0f : fabsf(z);
-            return fmaf(-a, normal_tail(z).tail, z > 0.0f ? z : 0.0f);
-        } else {
-            return z == -INFINITY ? 0.0f : z * (0.5f * erfcf(-z * SQRT_HALF));
-        }
-    }
-    return z < -100.0f ? 0.0f : z * sigmoid_of<FAST>(z);
+    if constexpr (FAST) return activate_fast(make_float2(z, z), kind).x;
+    else return activate_exact(z, kind);
 }
 template <bool FAST> __device__ __forceinline__ float activation_slope(float z, int kind) {
     if (kind == RGLRU_ACT_NONE) return 1.0f;
-    if (kind == RGLRU_ACT_GELU) {
-        const float zc = z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z;
-        if constexpr (FAST) {
-            const Normal n = normal_tail(zc);
-            return fmaf(zc * INV_SQRT_2PI, n.density, zc > 0.0f ? 1.0f - n.tail : n.tail);
-        } else {
-            return fmaf(zc * INV_SQRT_2PI, expf(-0.5f * zc * zc), 0.5f * erfcf(-zc * SQRT_HALF));
-        }
-    }
-    const float zc = z > 100.0f ? 100.0f : z < -100.0f ? -100.0f : z, s = sigmoid_of<FAST>(zc);
-    return s * fmaf(zc, 1.0f - s, 1.0f);
+    if constexpr (FAST) return slope_fast(make_float2(z, z), kind).x;
+    else return slope_exact(z, kind);
 }
 
 template <typename IO, int VE> struct LinearVec {

@@ -34,12 +34,12 @@ struct GemmArgs {
     alignas(64) CUtensorMap tm_a, tm_b;   // [planes][rows][cols]
     int a_turned, b_turned, split_planes; // split_planes: six products of planes instead of one
     int M, N, NT, nx, ny;                 // tiles: nx along M, ny along N
-    int kblocks, vblocks, splits, per_split;   // vblocks: K blocks over all products
+    int kblocks, vblocks;                 // vblocks: K blocks over all products
+    int whole, splits, per_split;         // tiles whose K is one pair's work; of the others each is split
     long long out_m, out_n;               // distances between results along M and N
     int wide;                             // bytes a thread may store at once along N (32, 16, or 0: one value)
     LinearEpilogue e;
-    float *part;                          // [splits][out] fp32, or null: the epilogue here
-    long long part_stride;
+    float *part;                          // [tile - whole][split][256 x NT] fp32, along the results' innermost dimension
     uint32_t *status;
     unsigned long long spin_ns;
 };
@@ -62,7 +62,7 @@ template <typename IO> __device__ __forceinline__ void finish_one(const LinearEp
     st1<IO>(e.y, o, activate<sizeof(IO) == 2>(z, e.activation) + (e.residual ? ld1<IO>(e.residual, o) : 0.0f));
 }
 // 32 neighbouring results of row m, v, to their place: a thread has a row, and writes whole sectors of it
-template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs &p, float *part, long long m, int n0, float *v) {
+template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs &p, long long m, int n0, float *v) {
     const long long o = m * p.out_m + n0;
     const LinearEpilogue &e = p.e;
     auto store_f32 = [&](float *dst) {
@@ -73,12 +73,10 @@ template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             if (n0 + j >= p.N) continue;
-            if (part) part[o + j] = v[j];
-            else finish_one<IO>(e, o + j, v[j] + (e.bias ? e.bias[n0 + j] : 0.0f));
+            finish_one<IO>(e, o + j, v[j] + (e.bias ? e.bias[n0 + j] : 0.0f));
         }
         return;
     }
-    if (part) { store_f32(part + o); return; }
     if (e.bias) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -108,7 +106,14 @@ template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs
     if (e.preact) store(e.preact);
     if (e.activation != RGLRU_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = activate<sizeof(IO) == 2>(v[j], e.activation);
+        for (int j = 0; j < 32; j += 2) {
+            if constexpr (sizeof(IO) == 2) {
+                const float2 y = activate_fast(make_float2(v[j], v[j + 1]), e.activation);
+                v[j] = y.x; v[j + 1] = y.y;
+            } else {
+                v[j] = activate<false>(v[j], e.activation); v[j + 1] = activate<false>(v[j + 1], e.activation);
+            }
+        }
     }
     if (e.residual) {
         constexpr int VE = 16 / sizeof(IO);
@@ -123,14 +128,13 @@ template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs
     store(e.y);
 }
 // 32 results of row m where neighbouring rows are neighbours in memory (tokens along N): lanes write side by side
-template <typename IO> __device__ __forceinline__ void finish_column(const GemmArgs &p, float *part, long long m, int n0, const float *v) {
-    const float b = p.e.bias && !part ? p.e.bias[m] : 0.0f;
+template <typename IO> __device__ __forceinline__ void finish_column(const GemmArgs &p, long long m, int n0, const float *v) {
+    const float b = p.e.bias ? p.e.bias[m] : 0.0f;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
         if (n0 + j >= p.N) continue;
         const long long o = m + (n0 + j) * p.out_n;
-        if (part) part[o] = v[j];
-        else finish_one<IO>(p.e, o, v[j] + b);
+        finish_one<IO>(p.e, o, v[j] + b);
     }
 }
 
@@ -151,7 +155,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_ctarank();
     const unsigned long long spin = p.spin_ns;
-    const int ntiles = p.nx * p.ny * p.splits, pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+    const int ntiles = p.whole + (p.nx * p.ny - p.whole) * p.splits, pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
 
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(BAR_FULL(s), 1); mbar_init(BAR_EMPTY(s), 1); }
@@ -170,11 +174,12 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
     bool ok = true;
     dependency_wait();
 
-    // tile -> (m, n, split); n fastest, so that the pairs at work at a time share rows of A, then splits of the same tile
-    struct Tile { int m, n, v0, v1; };
+    // unit of work -> (m, n, K blocks); n fastest, so that the pairs at work at a time share rows of A
+    struct Tile { int m, n, v0, v1, part; };
     auto tile_at = [&](int t) {
-        const int s = t % p.splits, xy = t / p.splits;
-        return Tile{xy / p.ny * 256, xy % p.ny * p.NT, s * p.per_split, min(p.vblocks, (s + 1) * p.per_split)};
+        if (t < p.whole) return Tile{t / p.ny * 256, t % p.ny * p.NT, 0, p.vblocks, -1};
+        const int u = t - p.whole, s = u % p.splits, xy = p.whole + u / p.splits;
+        return Tile{xy / p.ny * 256, xy % p.ny * p.NT, s * p.per_split, min(p.vblocks, (s + 1) * p.per_split), p.splits > 1 ? u : -1};
     };
 
     if (warp == 0) {
@@ -239,11 +244,23 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
             const Tile tl = tile_at(t);
             const long long m = tl.m + (long long)rank * 128 + q * 32 + lane;
             const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
-            float *part = p.part ? p.part + t % p.splits * p.part_stride : nullptr;
             auto finish = [&](int n0, float *v) {
                 if (m >= p.M || n0 >= p.N) return;
-                if (p.out_n == 1) finish_row<IO>(p, part, m, n0, v);
-                else finish_column<IO>(p, part, m, n0, v);
+                if (tl.part >= 0) {   // partial sums: whole tiles, in the order that the results have
+                    const int row = (int)(m - tl.m), col = n0 - tl.n;
+                    float *to = p.part + (size_t)tl.part * 256 * p.NT;
+                    if (p.out_n == 1) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) *(float4 *)(to + row * p.NT + col + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) to[(col + j) * 256 + row] = v[j];
+                    }
+                } else if (p.out_n == 1) {
+                    finish_row<IO>(p, m, n0, v);
+                } else {
+                    finish_column<IO>(p, m, n0, v);
+                }
             };
             if constexpr (DRAIN) {
                 float sum[2][32] = {};
@@ -304,29 +321,31 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
     if (warp == 1) tmem_dealloc2(tmem, 512);
 }
 
-// Sums over the splits of K in a fixed order, and the epilogue
+// Sums over the splits of K in a fixed order, and the epilogue, of the tiles that are split.  A thread has four neighbours of a tile.
 struct FinishArgs {
-    long long count, stride;
-    int N, splits;
+    int M, N, NT, ny, whole, splits;
+    long long out_m, out_n;
     const float *part;
     LinearEpilogue e;
 };
-template <typename IO, int VE> __global__ void __launch_bounds__(256) linear_finish_kernel(FinishArgs a) {
+template <typename IO> __global__ void __launch_bounds__(256) linear_finish_kernel(FinishArgs a) {
     dependency_wait();
-    const long long o = ((long long)blockIdx.x * 256 + threadIdx.x) * VE;
-    if (o < a.count) {
-        float z[VE] = {};
-        for (int s = 0; s < a.splits; ++s) {
-            if constexpr (VE == 4) {
-                const float4 v = *(const float4 *)(a.part + s * a.stride + o);
-                z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w;
-            } else {
-                z[0] += a.part[s * a.stride + o];
-            }
+    const int quads = 64 * a.NT, quad = (blockIdx.x % (quads / 256)) * 256 + threadIdx.x;
+    const int tile = blockIdx.x / (quads / 256), xy = a.whole + tile, inner = a.out_n == 1 ? a.NT : 256;
+    const int at = quad * 4, i = at / inner, j = at % inner;   // j along the results' innermost dimension
+    const int m = xy / a.ny * 256 + (a.out_n == 1 ? i : j), n = xy % a.ny * a.NT + (a.out_n == 1 ? j : i);
+    if (m < a.M && n < a.N) {
+        const float *p = a.part + (size_t)tile * a.splits * 256 * a.NT + at;
+        float z[4] = {};
+        for (int s = 0; s < a.splits; ++s, p += 256 * a.NT) {
+            const float4 v = *(const float4 *)p;
+            z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w;
         }
-        const int n = (int)(o % a.N);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) finish_one<IO>(a.e, o + e, z[e] + (a.e.bias ? a.e.bias[n + e] : 0.0f));
+        for (int e = 0; e < 4; ++e) {
+            const int me = m + (a.out_n == 1 ? 0 : e), ne = n + (a.out_n == 1 ? e : 0);
+            if (me < a.M && ne < a.N) finish_one<IO>(a.e, me * a.out_m + ne * a.out_n, z[e] + (a.e.bias ? a.e.bias[a.out_n == 1 ? ne : me] : 0.0f));
+        }
     }
     dependency_trigger();
 }
@@ -386,7 +405,7 @@ template <typename IO> __global__ void __launch_bounds__(256) linear_pack_kernel
 // ---- plan
 struct Plan {
     bool swapped, pack_a, pack_b;   // swapped: the caller's B is the kernel's A
-    int NT, nx, ny, kblocks, vblocks, splits, per_split;
+    int NT, nx, ny, kblocks, vblocks, whole, splits, per_split;
     size_t a_bytes, b_bytes, part_bytes;
 };
 inline bool f32(const LinearProduct &g) { return g.io == RGLRU_F32; }
@@ -398,25 +417,30 @@ Plan make_plan(const LinearProduct &g) {
     const LinearOperand &a = p.swapped ? g.b : g.a, &b = p.swapped ? g.a : g.b;
     p.kblocks = (int)((g.K + 63) / 64);
     p.vblocks = p.kblocks * (f32(g) ? PRODUCTS : 1);
-    // The tile width and the splits of K that take the busiest pair the fewest cycles: a K block costs about 256 + NT of them (copies
-    // out of L2 and products), a tile some 200 more, a split its partial results' way to memory and back and another launch.
+    // Whole rounds of pairs take a tile each; the tiles of the last, partly filled round are split along K over all pairs.  The tile width and
+    // the splits are those that take the busiest pair the fewest cycles: a K block costs about 256 + NT of them (copies out of L2 and
+    // products), a tile some 200 more, a split its partial results' way to memory and back and another launch.
     double best = 0;
     for (int nt : {256, 128, 64, 32}) {
         if ((f32(g) && nt > 128) || (b.turned && nt < 128)) continue;   // registers of the sums; copies 64 values wide
-        const long long nx = (M + 255) / 256, ny = (N + nt - 1) / nt;
+        const long long nx = (M + 255) / 256, ny = (N + nt - 1) / nt, tiles = nx * ny, whole = tiles / PAIRS * PAIRS, rest = tiles - whole;
+        const double block = 256 + nt;
         for (int s = 1; s <= 32 && s <= p.vblocks; ++s) {
             const int per = (p.vblocks + s - 1) / s;
-            if ((p.vblocks + per - 1) / per != s) continue;
-            double cost = (double)((nx * ny * s + PAIRS - 1) / PAIRS) * ((double)per * (256 + nt) + 200);
-            if (s > 1) cost += 3000 + (double)s * M * N * 8 / 2000;
-            if (best == 0 || cost < best) { best = cost; p.NT = nt; p.nx = (int)nx; p.ny = (int)ny; p.splits = s; p.per_split = per; }
+            if ((p.vblocks + per - 1) / per != s || (rest == 0 && s > 1)) continue;
+            double cost = (double)(whole / PAIRS) * (p.vblocks * block + 200) + (double)((rest * s + PAIRS - 1) / PAIRS) * (per * block + 200);
+            if (s > 1) cost += 3000 + (double)rest * s * 256 * nt * 8 / 2000;
+            if (best == 0 || cost < best) {
+                best = cost;
+                p.NT = nt; p.nx = (int)nx; p.ny = (int)ny; p.whole = (int)(s > 1 ? whole : tiles); p.splits = s; p.per_split = per;
+            }
         }
     }
     p.pack_a = f32(g) || a.cols % 8 != 0;
     p.pack_b = f32(g) || b.cols % 8 != 0;
     p.a_bytes = p.pack_a ? packed_bytes(a, f32(g)) : 0;
     p.b_bytes = p.pack_b ? packed_bytes(b, f32(g)) : 0;
-    p.part_bytes = p.splits > 1 ? up256((size_t)p.splits * g.M * g.N * sizeof(float)) : 0;
+    p.part_bytes = (size_t)((long long)p.nx * p.ny - p.whole) * p.splits * 256 * p.NT * sizeof(float);
     return p;
 }
 
@@ -485,15 +509,14 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
     a.a_turned = oa.turned; a.b_turned = ob.turned; a.split_planes = f32(g);
     a.M = (int)(p.swapped ? g.N : g.M); a.N = (int)(p.swapped ? g.M : g.N);
     a.NT = p.NT; a.nx = p.nx; a.ny = p.ny;
-    a.kblocks = p.kblocks; a.vblocks = p.vblocks; a.splits = p.splits; a.per_split = p.per_split;
+    a.kblocks = p.kblocks; a.vblocks = p.vblocks; a.whole = p.whole; a.splits = p.splits; a.per_split = p.per_split;
     a.out_m = p.swapped ? 1 : g.N; a.out_n = p.swapped ? g.N : 1;
     a.e = g.e;
-    a.part = p.splits > 1 ? (float *)(at + p.a_bytes + p.b_bytes) : nullptr;
-    a.part_stride = g.M * g.N;
-    const int per16 = 16 / (p.splits > 1 ? 4 : (int)io_bytes(g.io));
+    a.part = (float *)(at + p.a_bytes + p.b_bytes);
+    const int per16 = 16 / (int)io_bytes(g.io);
     a.wide = g.N % per16 != 0 ? 0 : g.N % (2 * per16) == 0 && aligned(g.e.y, 32) && aligned(g.e.preact, 32) ? 32 : 16;
     a.status = status; a.spin_ns = g_spin_limit_ns;
-    const long long tiles = (long long)p.nx * p.ny * p.splits;
+    const long long split = (long long)p.nx * p.ny - p.whole, tiles = p.whole + split * p.splits;
     if (tiles > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[2];
@@ -504,14 +527,9 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
     cfg.gridDim = dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = SMEM_ALLOC; cfg.stream = st;
     cfg.attrs = attr; cfg.numAttrs = 2;
     e = f32(g) ? cudaLaunchKernelEx(&cfg, linear_gemm_kernel<float>, a) : cudaLaunchKernelEx(&cfg, linear_gemm_kernel<__nv_bfloat16>, a);
-    if (e != cudaSuccess || p.splits == 1) return e;
-    const bool vec = g.N % 4 == 0;
-    const FinishArgs f{g.M * g.N, a.part_stride, (int)g.N, p.splits, a.part, g.e};
-    const long long blocks = (f.count / (vec ? 4 : 1) + 255) / 256;
-    if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-    auto kernel = f32(g) ? (vec ? linear_finish_kernel<float, 4> : linear_finish_kernel<float, 1>)
-                         : (vec ? linear_finish_kernel<__nv_bfloat16, 4> : linear_finish_kernel<__nv_bfloat16, 1>);
-    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(256), 0, st, f);
+    if (e != cudaSuccess || split == 0) return e;
+    const FinishArgs f{a.M, a.N, p.NT, p.ny, p.whole, p.splits, a.out_m, a.out_n, a.part, g.e};
+    return launch_dependent(f32(g) ? linear_finish_kernel<float> : linear_finish_kernel<__nv_bfloat16>, dim3((unsigned)(split * (p.NT / 4))), dim3(256), 0, st, f);
 }
 
 }  // namespace rglru
