@@ -162,7 +162,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
     } else if (warp == COPY_WARP) {
         reg_dec<48>();
         // ---- copies: k and v one chunk ahead of q
-        if (lane == 0) {
+        if (elect_one()) {
             auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
             auto tile = [&](int which, const Step &st, int width, uint32_t to, int bar) {
                 const int blocks = width > 64 ? 2 : 1;
@@ -191,7 +191,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         reg_dec<48>();
         // ---- products
         // Waits never suspend the thread: what it waits for is tens of cycles away, waking up takes hundreds.
-        if (lane == 0) {
+        if (elect_one()) {
             auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); };
             // Descriptors are counted on from step to step (16 bytes are one unit of their address field): held for all steps at once they
             // would not fit this warpgroup's registers.

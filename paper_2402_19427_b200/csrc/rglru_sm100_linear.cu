@@ -21,11 +21,11 @@ namespace {
 using namespace ptx;
 
 constexpr int THREADS = 320;              // TMA warp, MMA warp, eight epilogue warps
-constexpr int STAGES = 6;
-constexpr uint32_t A_BYTES = 128 * 128, B_BYTES = 128 * 128, STAGE = A_BYTES + B_BYTES;   // a CTA's share of a K block of 64 bf16
+constexpr uint32_t A_BYTES = 128 * 128, RING = 7 * 2 * A_BYTES;   // a CTA's 128 rows of a K block of 64 bf16; all stages
+constexpr int MAX_STAGES = 12;            // a stage is A_BYTES and 64 NT bytes of B: 7 of NT = 256, 12 of NT = 32
 constexpr uint32_t MN_BLOCK = 64 * 128;   // one copy of 64 K rows x 64 values of an operand turned
-constexpr uint32_t SMEM_BAR = STAGES * STAGE;
-constexpr uint32_t SMEM_TOTAL = SMEM_BAR + (2 * STAGES + 4) * 8 + 16, SMEM_ALLOC = SMEM_TOTAL + 1024;
+constexpr uint32_t SMEM_BAR = RING;
+constexpr uint32_t SMEM_TOTAL = SMEM_BAR + (2 * MAX_STAGES + 4) * 8 + 16, SMEM_ALLOC = SMEM_TOTAL + 1024;
 constexpr int PAIRS = 74;                 // the plan, and with it the workspace, does not depend on the device
 constexpr int PLANES = 4, PRODUCTS = 6;   // fp32: nearest, the same with zeros for what is not finite, second, third
 __device__ constexpr uint8_t PLANE_A[PRODUCTS] = {3, 1, 2, 2, 1, 0}, PLANE_B[PRODUCTS] = {1, 3, 2, 1, 2, 0};
@@ -35,6 +35,7 @@ struct GemmArgs {
     int a_turned, b_turned, split_planes; // split_planes: six products of planes instead of one
     int M, N, NT, nx, ny;                 // tiles: nx along M, ny along N
     int kblocks, vblocks;                 // vblocks: K blocks over all products
+    int stages;
     int whole, splits, per_split;         // tiles whose K is one pair's work; of the others each is split
     long long out_m, out_n;               // distances between results along M and N
     int wide;                             // bytes a thread may store at once along N (32, 16, or 0: one value)
@@ -147,18 +148,19 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
     uint8_t *smem = smem_raw + (base - raw_addr);
     const uint32_t bar0 = base + SMEM_BAR;
     auto BAR_FULL = [&](int s) { return bar0 + 8u * s; };
-    auto BAR_EMPTY = [&](int s) { return bar0 + 8u * (STAGES + s); };
-    auto BAR_ACCFULL = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
-    auto BAR_ACCEMPTY = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
-    uint32_t *tmem_base_s = (uint32_t *)(smem + SMEM_BAR + (2 * STAGES + 4) * 8);
+    auto BAR_EMPTY = [&](int s) { return bar0 + 8u * (MAX_STAGES + s); };
+    auto BAR_ACCFULL = [&](int a) { return bar0 + 8u * (2 * MAX_STAGES + a); };
+    auto BAR_ACCEMPTY = [&](int a) { return bar0 + 8u * (2 * MAX_STAGES + 2 + a); };
+    uint32_t *tmem_base_s = (uint32_t *)(smem + SMEM_BAR + (2 * MAX_STAGES + 4) * 8);
     volatile int *abort_flag = (volatile int *)(tmem_base_s + 1);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_ctarank();
     const unsigned long long spin = p.spin_ns;
-    const int ntiles = p.whole + (p.nx * p.ny - p.whole) * p.splits, pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+    const int ntiles = p.whole + (p.nx * p.ny - p.whole) * p.splits, pair = blockIdx.x >> 1, npairs = gridDim.x >> 1, stages = p.stages;
+    const uint32_t stage_bytes = A_BYTES + (uint32_t)p.NT * 64u;
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(BAR_FULL(s), 1); mbar_init(BAR_EMPTY(s), 1); }
+        for (int s = 0; s < stages; ++s) { mbar_init(BAR_FULL(s), 1); mbar_init(BAR_EMPTY(s), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(BAR_ACCFULL(a), 1); mbar_init(BAR_ACCEMPTY(a), 16); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -183,21 +185,21 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
     };
 
     if (warp == 0) {
-        if (lane == 0) {
-            int kbg = 0;   // K blocks so far, over all tiles
+        if (elect_one()) {
+            int s = 0;   // stage of the ring, and its turn
+            uint32_t turn = 0;
             const int brows = p.NT / 2;
             const uint32_t tx = 2 * (A_BYTES + (uint32_t)brows * 128u);   // both CTAs' bytes
             for (int t = pair; t < ntiles && ok; t += npairs) {
                 const Tile tl = tile_at(t);
                 const int ma = tl.m + (int)rank * 128, nb = tl.n + (int)rank * brows;
-                for (int v = tl.v0; v < tl.v1; ++v, ++kbg) {
-                    const int s = kbg % STAGES;
-                    ok = mbar_wait(BAR_EMPTY(s), ((kbg / STAGES) & 1) ^ 1, spin, abort_flag);
+                for (int v = tl.v0; v < tl.v1; ++v) {
+                    ok = mbar_wait_spin(BAR_EMPTY(s), turn ^ 1, spin, abort_flag);
                     if (!ok) break;
                     if (rank == 0) mbar_expect_tx(BAR_FULL(s), tx);
                     const int prod = p.split_planes ? v / p.kblocks : 0, k0 = (v - prod * p.kblocks) * 64;
                     const int pa = p.split_planes ? PLANE_A[prod] : 0, pb = p.split_planes ? PLANE_B[prod] : 0;
-                    const uint32_t a_dst = base + s * STAGE, b_dst = a_dst + A_BYTES;
+                    const uint32_t a_dst = base + s * stage_bytes, b_dst = a_dst + A_BYTES;
                     if (p.a_turned) {
                         tma_load_3d_pair(a_dst, &p.tm_a, ma, k0, pa, BAR_FULL(s));
                         tma_load_3d_pair(a_dst + MN_BLOCK, &p.tm_a, ma + 64, k0, pa, BAR_FULL(s));
@@ -209,30 +211,32 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
                     } else {
                         tma_load_3d_pair(b_dst, &p.tm_b, k0, nb, pb, BAR_FULL(s));
                     }
+                    if (++s == stages) { s = 0; turn ^= 1; }
                 }
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             const uint32_t idesc = instruction(256, p.NT, p.a_turned, p.b_turned);
-            int kbg = 0, it = 0;   // it: accumulators begun
+            int s = 0, it = 0;   // it: accumulators begun
+            uint32_t turn = 0;
             for (int t = pair; t < ntiles && ok; t += npairs) {
                 const Tile tl = tile_at(t);
-                for (int v = tl.v0; v < tl.v1 && ok; ++v, ++kbg) {
+                for (int v = tl.v0; v < tl.v1 && ok; ++v) {
                     const int within = DRAIN ? (v - tl.v0) % DRAIN_BLOCKS : v - tl.v0, acc = it & 1;
-                    if (within == 0) ok = mbar_wait_cl(BAR_ACCEMPTY(acc), ((it >> 1) & 1) ^ 1, spin, abort_flag);
-                    const int s = kbg % STAGES;
-                    ok = ok && mbar_wait_cl(BAR_FULL(s), (kbg / STAGES) & 1, spin, abort_flag);
+                    if (within == 0) ok = mbar_wait_spin(BAR_ACCEMPTY(acc), ((it >> 1) & 1) ^ 1, spin, abort_flag);
+                    ok = ok && mbar_wait_spin(BAR_FULL(s), turn, spin, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t a = base + s * STAGE, b = a + A_BYTES, d = tmem + acc * 256;
+                    const uint32_t a = base + s * stage_bytes, b = a + A_BYTES, d = tmem + acc * 256;
 #pragma unroll
                     for (int k = 0; k < 4; ++k)   // 16 of K an instruction: 32 bytes along a row, or 16 rows
                         mma_ss2(d, p.a_turned ? make_desc_sw128_mn(a + k * 2048, MN_BLOCK) : make_desc_sw128(a + k * 32),
                                 p.b_turned ? make_desc_sw128_mn(b + k * 2048, MN_BLOCK) : make_desc_sw128(b + k * 32), idesc, (within | k) != 0);
                     tc_commit2(BAR_EMPTY(s), 3);
                     if (v + 1 == tl.v1 || (DRAIN && within + 1 == DRAIN_BLOCKS)) { tc_commit2(BAR_ACCFULL(acc), 3); ++it; }
+                    if (++s == stages) { s = 0; turn ^= 1; }
                 }
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
@@ -508,6 +512,7 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
     if ((e = place(ob, g.io, p.pack_b, at + p.a_bytes, p.NT / 2, &a.tm_b, st)) != cudaSuccess) return e;
     a.a_turned = oa.turned; a.b_turned = ob.turned; a.split_planes = f32(g);
     a.M = (int)(p.swapped ? g.N : g.M); a.N = (int)(p.swapped ? g.M : g.N);
+    a.stages = (int)(RING / (A_BYTES + (uint32_t)p.NT * 64u));
     a.NT = p.NT; a.nx = p.nx; a.ny = p.ny;
     a.kblocks = p.kblocks; a.vblocks = p.vblocks; a.whole = p.whole; a.splits = p.splits; a.per_split = p.per_split;
     a.out_m = p.swapped ? 1 : g.N; a.out_n = p.swapped ? g.N : 1;

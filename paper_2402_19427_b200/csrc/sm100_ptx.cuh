@@ -146,6 +146,13 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
                  ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
 }
+// One thread of the warp.  The compiler knows that a branch on it leaves a single thread, and reads the operands of tcgen05 and TMA instructions
+// straight into uniform registers there; behind `lane == 0` it loops over the lanes that might be active, some 80 cycles an instruction.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
 // Blocks that wait for one another's carry records.  A block marks the record it will write first when it starts, with a word that no
 // published record holds.  The limit of a wait for records counts from when every block waited for has left its mark: blocks that
 // other work on the GPU keeps off the SMs are no failure (with a limit of their own all the same, CARRY_START_LIMITS times as long).
