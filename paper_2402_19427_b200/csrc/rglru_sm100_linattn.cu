@@ -8,10 +8,14 @@
 // and out = Y + decay X, S <- d^n S + U.  The state itself stays in fp32 registers from chunk to chunk.  It is an output of the call and
 // has to be as exact as fp32 sums are, so the decayed k enters U as three bf16 values that add up to it; P and S enter once.
 //
-// Bound by memory: a chunk of 128 x 128 moves 128 KB, 3.0 us of an SM's share of the measured copy rate; the products take 1.7 us.  One block
-// an SM: 224 KB of q, k (twice), v, S, a ring for the planes of k, and outputs on their way.  Each tile is requested again as soon as its last reader is done: q after the
-// far product, k after the scores and planes, v at the chunk's end.  Warps: four turn P into the operand of the near product (in tensor memory,
-// over the scores), look through v and write the outputs, eight keep the state, eight make the planes, one copies, one issues.
+// A chunk of 128 x 128 moves 128 KB, 3.0 us of an SM's share of the measured copy rate; its 48 matrix instructions take 64 cycles each, 1.6 us.  It takes
+// 4.4 to 4.6 us with all SMs at work: the way from one state product to the next (the state's update, the planes of the next k, its
+// scores, each handed on through a barrier some 300 to 500 cycles after it is ready) is what bounds it, not one of its resources (41 % of the issue
+// slots, 45 % of the shared-memory pipe).  One block an SM: 224 KB of q, k and v (twice), S and planes.  A tile is requested again as soon as its last
+// reader is done: q after the far product, k and v after the state product.  Warps: four look through v and turn P into the operand of
+// the near product (in tensor memory, over the scores), four write the outputs, eight keep the state, eight make the planes, one copies, one issues.
+// Outputs go from registers to memory, 32 bytes a thread: staged in shared memory for a tiled copy they held v's place for
+// another 4000 cycles a chunk.
 //
 // Blocks share the chunks of all (role, sequence, head) evenly, in order; a block that begins inside a sequence takes the state before it
 // from the sums that a first launch (planes and state product only) leaves for the stretches in front of it.
@@ -27,9 +31,10 @@ namespace {
 using namespace ptx;
 
 constexpr int CH = 128;                          // tokens a chunk
-// Warpgroups of four: weights and outputs, state (two), planes (two), copies and products.  768 threads start with 80 registers each;
-// 96 + 2 x 120 + 2 x 48 + 48 are the same 480.
-constexpr int P_WARPS = 4, S_WARPS = 8, K_WARPS = 8, COPY_WARP = P_WARPS + S_WARPS + K_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (COPY_WARP + 4) * 32;
+// Warpgroups of four: weights, outputs, state (two), planes (two), copies and products.  896 threads start with 72 registers each;
+// 2 x 80 + 2 x 112 + 2 x 40 + 40 are the same 504.
+constexpr int P_WARPS = 4, O_WARPS = 4, S_WARPS = 8, K_WARPS = 8, S_FIRST = P_WARPS + O_WARPS, K_FIRST = S_FIRST + S_WARPS;
+constexpr int COPY_WARP = K_FIRST + K_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (COPY_WARP + 4) * 32;
 constexpr uint32_t BLOCK = 128 * 128;            // 128 rows of 64 bf16
 // The planes of the decayed k are made 32 tokens (a piece) at a time.  The first plane takes the place of the k it is made from; the others
 // of pieces 0 and 1 have slots of their own, those of pieces 2 and 3 lie in S's place, which is free from the far product to the next S.
@@ -39,7 +44,7 @@ constexpr uint32_t TILE = 2 * BLOCK;
 constexpr uint32_t SM_Q = 0, SM_K = TILE, SM_V = SM_K + 2 * TILE, SM_S = SM_V + 2 * TILE, SM_PLANES = SM_S + TILE, SM_BAR = SM_PLANES + 2 * SLOT;
 __host__ __device__ constexpr uint32_t slot_at(int piece) { return piece < 2 ? SM_PLANES + piece * SLOT : SM_S + (piece - 2) * SLOT; }
 static_assert(2 * SLOT <= TILE, "slots in S's place");
-enum { QF, QE, SC, PR, DSF, SR, OF, OE, KF, KE = KF + 2, VF = KE + 2, VK = VF + 2, VE = VK + 2, PLF = VE + 2, NBAR = PLF + PIECES };   // two of each for the two tiles of k and v
+enum { QF, QE, SC, PR, DSF, UR, SR, OE, KF, VF = KF + 2, VK = VF + 2, KVE = VK + 2, PLE = KVE + 2, PLF = PLE + 1, NBAR = PLF + PIECES };   // two of each for the two tiles of k and v
 constexpr uint32_t SM_TMEM = SM_BAR + NBAR * 8, SM_BAD = SM_TMEM + 16,
                    SM_TOTAL = SM_BAD + 8 * 132, SM_ALLOC = SM_TOTAL + 1024;
 static_assert(SM_ALLOC <= 232448, "shared memory of a block");
@@ -47,7 +52,7 @@ constexpr uint32_t TM_P = 0, TM_Y = 128, TM_X = 256, TM_U = 384;   // tensor-mem
 constexpr int WALKERS = 148;                     // the plan, and with it the workspace, does not depend on the device
 
 struct WalkArgs {
-    alignas(64) CUtensorMap tm[3][4];            // q, k, v and the outputs of each role: [B][T][H][width]
+    alignas(64) CUtensorMap tm[3][3];            // q, k, v of each role: [B][T][H][width]
     MixArgs m;
     int units, chunks;                           // (role, sequence, head), chunks of each
     int walkers;
@@ -92,6 +97,7 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+__device__ __forceinline__ __nv_bfloat162 larger(__nv_bfloat162 top, uint32_t w) { return __hmax2_nan(top, __habs2(*(const __nv_bfloat162 *)&w)); }
 // Bits 15 and 31 of the result: whether the two bf16 of w are infinite or NaN (all bits of the exponent set)
 __device__ __forceinline__ uint32_t no_numbers(uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; }
 
@@ -119,6 +125,12 @@ __device__ __forceinline__ void mend_piece(uint32_t addr, int column, uint32_t t
     *(volatile uint32_t *)(bad + 32) = 1u;
 }
 
+__device__ __forceinline__ void load_tile(const WalkArgs &p, int which, const Step &st, int width, uint32_t to, uint32_t bar) {
+    const int blocks = width > 64 ? 2 : 1;
+    mbar_expect_tx(bar, blocks * BLOCK);
+    for (int j = 0; j < blocks; ++j) tma_load_4d(to + j * BLOCK, &p.tm[st.role][which], j * 64, st.h, st.t0, st.b, bar);
+}
+
 // STATE_ONLY: the sums U of a block's last stretch, for the blocks that go on in the same sequence
 template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kernel(const __grid_constant__ WalkArgs p) {
     extern __shared__ uint8_t smem_raw[];
@@ -133,8 +145,8 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
 
     if (tid == 0) {
         for (int i = 0; i < NBAR; ++i) {
-            const bool by_p = i == PR || i == OE || i == VK || i == VK + 1 || (!STATE_ONLY && (i == VE || i == VE + 1));
-            mbar_init(BAR(i), by_p ? P_WARPS : i == SR ? S_WARPS : i >= PLF ? K_WARPS : 1);
+            const bool by_four = i == PR || i == OE || i == VK || i == VK + 1;
+            mbar_init(BAR(i), by_four ? 4 : i == SR || i == UR ? S_WARPS : i >= PLF ? K_WARPS : 1);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -158,37 +170,30 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
 
     // (each role takes its registers in its own branch: behind a join, all code would get by with the fewest)
     if (warp > MMA_WARP) {
-        reg_dec<48>();
+        reg_dec<40>();
     } else if (warp == COPY_WARP) {
-        reg_dec<48>();
+        reg_dec<40>();
         // ---- copies: k and v one chunk ahead of q
         if (elect_one()) {
             auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
-            auto tile = [&](int which, const Step &st, int width, uint32_t to, int bar) {
-                const int blocks = width > 64 ? 2 : 1;
-                mbar_expect_tx(BAR(bar), blocks * BLOCK);
-                for (int j = 0; j < blocks; ++j) tma_load_4d(base + to + j * BLOCK, &p.tm[st.role][which], j * 64, st.h, st.t0, st.b, BAR(bar));
-            };
             Step st(p, first), ahead = st;
             auto load_kv = [&](int s) {
                 const MixRole &r = p.m.role[ahead.role];
                 const int k = s & 1;
-                const uint32_t before = (s >> 1 & 1) ^ 1;
-                if (!wait(KE + k, before)) return;
-                tile(1, ahead, r.dk, SM_K + k * TILE, KF + k);
-                if (!wait(VE + k, before)) return;
-                tile(2, ahead, r.dv, SM_V + k * TILE, VF + k);
+                if (!wait(KVE + k, (s >> 1 & 1) ^ 1)) return;
+                load_tile(p, 1, ahead, r.dk, base + SM_K + k * TILE, BAR(KF + k));
+                load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
                 ahead.next(p);
             };
             if (steps > 0) load_kv(0);
             for (int s = 0; s < steps && ok; ++s, st.next(p)) {
-                if (!STATE_ONLY && wait(QE, (s & 1) ^ 1)) tile(0, st, p.m.role[st.role].dk, SM_Q, QF);
+                if (!STATE_ONLY && wait(QE, (s & 1) ^ 1)) load_tile(p, 0, st, p.m.role[st.role].dk, base + SM_Q, BAR(QF));
                 if (ok && s + 1 < steps) load_kv(s + 1);
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp == MMA_WARP) {
-        reg_dec<48>();
+        reg_dec<40>();
         // ---- products
         // Waits never suspend the thread: what it waits for is tens of cycles away, waking up takes hundreds.
         if (elect_one()) {
@@ -231,59 +236,62 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                     for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, first_plane + k * 128, v + k * 128, id_ab, 1);
                     v += 256;
                 };
-                wait(SR, ph);
                 wait(VK + (s & 1), s >> 1 & 1);
+                wait(UR, ph ^ 1);
 #pragma unroll 1
                 for (int pc = 0; pc < PIECES; ++pc) {
-                    if (!STATE_ONLY && pc == 1) {   // the last outputs have been read by now
-                        wait(OE, ph ^ 1);
+                    if (!STATE_ONLY && pc == 1) {
+                        wait(SR, ph);
+                        wait(OE, ph ^ 1);   // the last outputs have been read
                         if (!ok) break;
                         tc_fence_after();
-                        uint64_t state = turned(SM_S, BLOCK);   // S as it lies: rows of 64 columns of v
+                        uint64_t rows = turned(SM_S, BLOCK);   // S as it lies: rows of 64 columns of v
 #pragma unroll 1
-                        for (int b = 0; b * 64 < r.dk; ++b, state += 4 * 128) {
+                        for (int b = 0; b * 64 < r.dk; ++b, rows += 4 * 128) {
                             const uint64_t q = kmajor(SM_Q + b * BLOCK);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_X, q + 2 * i, state + 128 * i, id_b, b | i);
+                            for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_X, q + 2 * i, rows + 128 * i, id_b, b | i);
                         }
                         tc_commit(BAR(QE));
+                    }
+                    if (pc == 2) tc_commit(BAR(PLE));   // the first two slots have been read
+                    if (!STATE_ONLY && pc == 2) {
+                        wait(PR, ph);
+                        if (!ok) break;
+                        tc_fence_after();
+                        uint64_t rows = turned(v_at, BLOCK);
+#pragma unroll 4
+                        for (int k = 0; k < 8; ++k, rows += 128) mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, rows, id_b, k);
                     }
                     piece(pc);
                     if (!ok) break;
                 }
                 if (!ok) break;
-                tc_commit(BAR(DSF));
-                tc_commit(BAR(KE + (s & 1)));
-                if (!STATE_ONLY) {
-                    wait(PR, ph);
-                    if (!ok) break;
-                    tc_fence_after();
-                    v = turned(v_at, BLOCK);
-#pragma unroll 4
-                    for (int k = 0; k < 8; ++k) mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, v + k * 128, id_b, k);
-                    tc_commit(BAR(OF));
-                }
-                if (STATE_ONLY) tc_commit(BAR(VE + (s & 1)));   // else the outputs leave through v's tile first
+                tc_commit(BAR(DSF));   // all of the step's products
+                tc_commit(BAR(KVE + (s & 1)));
                 st.next(p);
                 if (!STATE_ONLY && s + 1 < steps) scores(s + 1, p.m.role[st.role]);
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp < P_WARPS) {
-        reg_inc<96>();
-        // ---- what is no number in v; scores to weights, outputs: a thread has a row (a token)
+        reg_inc<80>();
+        // ---- what is no number in v; scores to weights: a thread has a row (a token)
         auto look_through = [&](int s, const Step &st) {
             const MixRole &r = p.m.role[st.role];
             const uint32_t tile = base + SM_V + (s & 1) * TILE;
-            ok = ok && warp_wait_held(BAR(VF + (s & 1)), s >> 1 & 1, spin, abort_flag);
+            ok = warp_wait_held(BAR(VF + (s & 1)), s >> 1 & 1, spin, abort_flag);
             if (!ok) return;
             const int rounds = r.dv > 64 ? 16 : 8;
-            uint32_t found = 0;
+            __nv_bfloat162 top[4] = {};   // the largest magnitudes, NaN above all
 #pragma unroll 8
             for (int k = 0; k < rounds; ++k) {
                 const uint4 v = lds128(tile + (k * P_WARPS * 32 + tid) * 16);
-                found |= no_numbers(v.x) | no_numbers(v.y) | no_numbers(v.z) | no_numbers(v.w);
+                top[0] = larger(top[0], v.x); top[1] = larger(top[1], v.y); top[2] = larger(top[2], v.z); top[3] = larger(top[3], v.w);
             }
+            uint32_t found = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) found |= no_numbers(*(const uint32_t *)&top[k]);
             if (found & 0x80008000u) {
                 for (int k = 0; k < rounds; ++k) {
                     const int at = k * P_WARPS * 32 + tid, vrow = (at >> 3) & 127, column = (at >> 10) * 64 + ((at & 7) ^ (vrow & 7)) * 8;
@@ -296,7 +304,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         };
         const int row = warp * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-        float ld = 0.0f, d1 = 0.0f, far = 0.0f;
+        float ld = 0.0f, d1 = 0.0f;
         Step st(p, first), ahead = st;
         if (steps > 0) look_through(0, ahead);
         for (int s = 0; s < steps && ok; ++s, st.next(p)) {
@@ -308,28 +316,26 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             const MixRole &r = p.m.role[st.role];
             const uint32_t ph = s & 1;
             const bool reverse = r.reverse;
-            const int i = reverse ? CH - 1 - row : row;
             if (st.fresh) {
                 ld = p.m.log_decay[st.h];
                 d1 = decay_power(ld, 1.0f);
-                far = r.si * decay_power(ld, (float)(i + r.first));
             }
             ok = warp_wait_held(BAR(SC), ph, spin, abort_flag);
             if (!ok) break;
             tc_fence_after();
             // Weights by multiplication, column after column away from the diagonal (so that they run into 0 and not out of infinity); a table
             // in shared memory would compete with the products' operands for its bandwidth.
-            const int own = reverse ? P_WARPS - 1 - warp : warp;
+            const int own = reverse ? 3 - warp : warp;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 const int cw = reverse ? 3 - c : c;   // the 32 columns' place in walking order
                 uint32_t w[16];
+                f32x2 v[16];
+                if (cw <= own) tmem_ld32(lanes + TM_P + c * 32, v);
                 if (cw > own) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) w[j] = 0u;
                 } else {
-                    f32x2 v[16];
-                    tmem_ld32(lanes + TM_P + c * 32, v);
                     if (cw == own) {   // chosen, not multiplied by 0: what is masked may be no number
                         tmem_ld_wait();
                         float run = r.sp;
@@ -373,70 +379,69 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(PR));
-
             if (s + 1 < steps) look_through(s + 1, ahead);
-            ok = ok && warp_wait_held(BAR(OF), ph, spin, abort_flag);
+        }
+        if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
+    } else if (warp < P_WARPS + O_WARPS) {
+        reg_inc<80>();
+        // ---- outputs: a thread has a row (a token)
+        const int quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        float far = 0.0f;
+        Step st(p, first);
+        for (int s = 0; !STATE_ONLY && s < steps && ok; ++s, st.next(p)) {
+            const MixRole &r = p.m.role[st.role];
+            const uint32_t ph = s & 1;
+            const int i = r.reverse ? CH - 1 - row : row;
+            if (st.fresh) far = r.si * decay_power(p.m.log_decay[st.h], (float)(i + r.first));
+            ok = warp_wait_held(BAR(DSF), ph, spin, abort_flag);
             if (!ok) break;
             tc_fence_after();
             const uint8_t *bad = (const uint8_t *)(bad_base + (s & 7) * 33);
             const bool any_bad = *(volatile const uint32_t *)(bad + 128) != 0;
-            // v's tile has been read: the outputs go through it, 16-byte pieces swizzled as the copies want them
-            const uint32_t stage = base + SM_V + (s & 1) * TILE + warp * 32 * 128;
+            const int t = st.t0 + row;
+            const bool there = t >= 0 && t < p.m.T;
+            __nv_bfloat16 *to = (__nv_bfloat16 *)r.o.p + st.b * r.o.batch + t * r.o.token + (long long)st.h * r.dv;
+            const bool wide = r.dv % 16 == 0 && (((size_t)r.o.p | (size_t)(r.o.token * 2) | (size_t)(r.o.batch * 2)) & 31) == 0;
 #pragma unroll 1
-            for (int c = 0; c < r.dv; c += 32) {
-                f32x2 y[16], x[16];
-                tmem_ld32(lanes + TM_Y + c, y);
-                tmem_ld32(lanes + TM_X + c, x);
+            for (int c = 0; c < r.dv; c += 16) {
+                f32x2 y[8], x[8];
+                tmem_ld16(lanes + TM_Y + c, y);
+                tmem_ld16(lanes + TM_X + c, x);
                 tmem_ld_wait();
-                if (c + 32 >= r.dv) {
+                if (c + 16 >= r.dv) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(BAR(OE));
                 }
-                uint32_t w[16];
+                uint32_t w[8];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
+                for (int j = 0; j < 8; ++j) {
                     y[j] = fma2(x[j], pack2(far, far), y[j]);
                     w[j] = pack_bf16(y[j].x, y[j].y);
                 }
                 if (any_bad) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
+                    for (int j = 0; j < 8; ++j) {
                         if (i >= bad[c + 2 * j]) w[j] = w[j] & 0xFFFF0000u | 0x7FC0u;
                         if (i >= bad[c + 2 * j + 1]) w[j] = w[j] & 0x0000FFFFu | 0x7FC00000u;
                     }
                 }
-#pragma unroll
-                for (int h = 0; h < 4; ++h)
-                    sts128(stage + c / 64 * BLOCK + lane * 128 + ((((c & 32) / 8 + h) ^ (lane & 7)) << 4), make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
-            }
-            fence_async_smem();
-            __syncwarp();
-            const int t0 = st.t0 + warp * 32;
-            if (t0 >= 0) {   // rows behind the last token are cut off by the copy
-                if (lane == 0 && t0 < p.m.T) {
-                    for (int j = 0; j * 64 < r.dv; ++j) tma_store_4d(&p.tm[st.role][3], j * 64, st.h, t0, st.b, stage + j * BLOCK);
-                    bulk_commit();
-                    bulk_wait_read0();
+                if (there) {
+                    if (wide) {
+                        st_global_v8(to + c, w);
+                    } else {
+                        *(uint4 *)(to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                        if (c + 8 < r.dv) *(uint4 *)(to + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
                 }
-            } else {         // the end of a reversed walk: a copy must not start in front of the first token
-                for (int k = lane >> 4; k < 32; k += 2) {
-                    const int c = lane & 15;
-                    if (t0 + k >= 0 && c * 8 < r.dv)
-                        *(uint4 *)((__nv_bfloat16 *)r.o.p + st.b * r.o.batch + (t0 + k) * r.o.token + (long long)st.h * r.dv + c * 8) =
-                            lds128(stage + c / 8 * BLOCK + k * 128 + ((c & 7 ^ k & 7) << 4));
-                }
-                fence_async_smem();
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(BAR(VE + (s & 1)));
         }
-        if (lane == 0) bulk_wait0();
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
-    } else if (warp < P_WARPS + S_WARPS) {
-        reg_inc<120>();
+    } else if (warp < K_FIRST) {
+        reg_inc<112>();
         // ---- the state: a thread has row d of S and 64 columns
-        const int q = warp & 3, e0 = (warp - P_WARPS) / 4 * 64, d = q * 32 + lane;
+        const int q = warp & 3, e0 = (warp - S_FIRST) / 4 * 64, d = q * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
         f32x2 S2[32];
         auto at = [&](int j) -> float & { return j & 1 ? S2[j / 2].y : S2[j / 2].x; };
@@ -479,8 +484,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                                                                pack_bf16(S2[4 * j + 2].x, S2[4 * j + 2].y), pack_bf16(S2[4 * j + 3].x, S2[4 * j + 3].y)));
         };
         auto handed_over = [&]() {
-            if (!STATE_ONLY) fence_async_smem();
-            tc_fence_before();
+            fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(BAR(SR));
         };
@@ -494,10 +498,11 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             if (st.fresh) {
                 ld = p.m.log_decay[st.h];
                 init_state(st, first + s);
-                if (!STATE_ONLY)
+                if (!STATE_ONLY) {
 #pragma unroll
                     for (int c = 0; c < 64; c += 16) put16(c);
-                handed_over();
+                    handed_over();
+                }
             }
             const float f = decay_power(ld, (float)st.n), su = r.su;
             const bool last_chunk = st.chunk == p.chunks - 1;
@@ -516,20 +521,23 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
 #pragma unroll
                     for (int j = 0; j < 8; ++j) S2[c / 2 + j] = fma2(pack2(f, f), S2[c / 2 + j], mul2(pack2(su, su), u[c / 16 & 1][j]));
                 }
-                if (!STATE_ONLY && !last_chunk) put16(c);
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(UR));
             if (*(volatile uint32_t *)(bad + 32)) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
                     if (((const uint8_t *)bad)[e0 + j] != 255) at(j) = __int_as_float(0x7FC00000);
-                if (!STATE_ONLY && !last_chunk)
-#pragma unroll
-                    for (int c = 0; c < 64; c += 16) put16(c);
             }
-            if (!last_chunk) handed_over();
+            if (!STATE_ONLY && !last_chunk) {
+#pragma unroll
+                for (int c = 0; c < 64; c += 16) put16(c);
+                handed_over();
+            }
             // The list of two steps ago has been read: by the outputs before they let the last step's go on, by the states before their SR.
             // It serves again in six steps, long after products that wait for this warp's SR.
-            if (warp == P_WARPS && s > 1) {
+            if (warp == S_FIRST && s > 1) {
                 uint32_t *old = bad_base + (s - 2 & 7) * 33;
                 if (*(volatile uint32_t *)(old + 32)) {
                     old[lane] = 0xFFFFFFFFu;
@@ -551,9 +559,9 @@ if (STATE_ONLY && steps > 0 && ok) {
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     } else {
-        reg_dec<48>();
+        reg_dec<40>();
         // ---- planes of the decayed k
-        const int k_tid = tid - (P_WARPS + S_WARPS) * 32;
+        const int k_tid = tid - K_FIRST * 32;
         float weight = 0.0f;
         int n_tokens = 0;
         Step st(p, first);
@@ -591,11 +599,13 @@ if (STATE_ONLY && steps > 0 && ok) {
                     x = fma2(bf2x(mid[i]), minus, x);
                     lo[i] = upper_halves(x);
                 }
-                if (pc == 0) {   // the last state product has read the slots, the scores k
-                    ok = warp_wait_held(BAR(DSF), ph ^ 1, spin, abort_flag);
+                // The last state product has read the slots, the scores k, and the far product S
+                if (pc == 0) {
+                    ok = warp_wait_held(BAR(PLE), ph ^ 1, spin, abort_flag);
                     if (!STATE_ONLY) ok = ok && warp_wait_held(BAR(SC), ph, spin, abort_flag);
+                } else if (pc == 2) {
+                    ok = STATE_ONLY ? warp_wait_held(BAR(DSF), ph ^ 1, spin, abort_flag) : warp_wait_held(BAR(QE), ph, spin, abort_flag);
                 }
-                if (!STATE_ONLY && pc == 2) ok = warp_wait_held(BAR(QE), ph, spin, abort_flag);   // the far product has read S
                 if (!ok) break;
                 if (mine) {
                     const uint32_t to = dst + slot_at(pc);
@@ -613,6 +623,7 @@ if (STATE_ONLY && steps > 0 && ok) {
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     }
+    __syncwarp();   // an elected thread and its warp: what follows is for whole warps
     dependency_trigger();
     if (*abort_flag) {   // let copies and MMAs in flight land before shared and tensor memory are given back
         const uint64_t tw = gtimer();
@@ -661,13 +672,13 @@ cudaError_t sm100_mix(const MixArgs &a, void *scratch, cudaStream_t st) {
     p.spin_ns = g_spin_limit_ns;
     for (int i = 0; i < a.roles; ++i) {
         const MixRole &r = a.role[i];
-        const MixTensor *t[4] = {&r.q, &r.k, &r.v, &r.o};
-        for (int j = 0; j < 4; ++j) {
+        const MixTensor *t[3] = {&r.q, &r.k, &r.v};
+        for (int j = 0; j < 3; ++j) {
             const uint64_t w = j < 2 ? r.dk : r.dv;
             // an axis of one element has no distance: any valid one
             const uint64_t token = a.T > 1 ? t[j]->token : w * a.H, batch = a.B > 1 ? t[j]->batch : w * a.H;
             const uint64_t dims[4] = {w, (uint64_t)a.H, (uint64_t)a.T, (uint64_t)a.B}, strides[3] = {w * 2, token * 2, batch * 2};
-            const uint32_t box[4] = {64, 1, j < 3 ? CH : 32u, 1};   // outputs leave warp by warp
+            const uint32_t box[4] = {64, 1, CH, 1};
             if (!encode_map16_4d(&p.tm[i][j], t[j]->p, dims, strides, box, true)) return cudaErrorNotSupported;
         }
     }

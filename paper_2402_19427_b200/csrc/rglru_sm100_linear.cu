@@ -313,6 +313,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
     }
+    __syncwarp();   // an elected thread and its warp: what follows is for whole warps
     dependency_trigger();
     if (*abort_flag) {   // let copies and MMAs in flight land before shared and tensor memory are given back
         const uint64_t tw = gtimer();
