@@ -147,7 +147,7 @@ struct DzArgs {
     void *dz;                 // null: only the sums (no activation: dz is dy)
     float *part;              // [row blocks][N] or null
 };
-template <typename IO, int VE> __global__ void __launch_bounds__(256) linear_dz_kernel(DzArgs a) {
+template <typename IO, int VE> __global__ void __launch_bounds__(256, 2) linear_dz_kernel(DzArgs a) {
     __shared__ float red[8][32 * VE];
     dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -155,29 +155,52 @@ template <typename IO, int VE> __global__ void __launch_bounds__(256) linear_dz_
     const long long r0 = (long long)blockIdx.y * a.rows, r1 = min(a.M, r0 + a.rows);
     float s[VE] = {};
     if (c < a.N) {
-#pragma unroll 4
-        for (long long r = r0 + warp; r < r1; r += 8) {
-            const long long o = r * a.N + c;
-            float g[VE];
-            LinearVec<IO, VE>::load((const IO *)a.dy + o, g);
-            if (a.activation != RGLRU_ACT_NONE) {
-                float z[VE];
-                LinearVec<IO, VE>::load((const IO *)a.preact + o, z);
-                if constexpr (sizeof(IO) == 2 && VE > 1) {
+        // Rows in batches, the next one's loads in flight while this one is computed
+        constexpr int BATCH = 4;
+        using Vec = LinearVec<IO, VE>;
+        typename Vec::Raw gs[BATCH], zs[BATCH];
+        auto load = [&](long long r) {
 #pragma unroll
-                    for (int e = 0; e < VE; e += 2) {
-                        const float2 d = slope_fast(make_float2(z[e], z[e + 1]), a.activation);
-                        g[e] *= d.x;
-                        g[e + 1] *= d.y;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) g[e] *= activation_slope<sizeof(IO) == 2>(z[e], a.activation);
-                }
-                if (a.dz) LinearVec<IO, VE>::store((IO *)a.dz + o, g);
+            for (int u = 0; u < BATCH; ++u) {
+                if (r + 8 * u >= r1) continue;
+                const long long o = (r + 8 * u) * a.N + c;
+                gs[u] = *(const typename Vec::Raw *)((const IO *)a.dy + o);
+                if (a.activation != RGLRU_ACT_NONE) zs[u] = *(const typename Vec::Raw *)((const IO *)a.preact + o);
             }
+        };
+        long long r = r0 + warp;
+        load(r);
+#pragma unroll 1
+        while (r < r1) {
+            typename Vec::Raw gn[BATCH], zn[BATCH];
+            const long long now = r;
 #pragma unroll
-            for (int e = 0; e < VE; ++e) s[e] += g[e];
+            for (int u = 0; u < BATCH; ++u) { gn[u] = gs[u]; zn[u] = zs[u]; }
+            load(r += 8 * BATCH);
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                if (now + 8 * u >= r1) continue;
+                float g[VE];
+                Vec::unpack(gn[u], g);
+                if (a.activation != RGLRU_ACT_NONE) {
+                    float z[VE];
+                    Vec::unpack(zn[u], z);
+                    if constexpr (sizeof(IO) == 2 && VE > 1) {
+#pragma unroll
+                        for (int e = 0; e < VE; e += 2) {
+                            const float2 d = mul2(make_float2(g[e], g[e + 1]), slope_fast(make_float2(z[e], z[e + 1]), a.activation));
+                            g[e] = d.x;
+                            g[e + 1] = d.y;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) g[e] *= activation_slope<sizeof(IO) == 2>(z[e], a.activation);
+                    }
+                    if (a.dz) Vec::store((IO *)a.dz + (now + 8 * u) * a.N + c, g);
+                }
+#pragma unroll
+                for (int e = 0; e < VE; ++e) s[e] += g[e];
+            }
         }
     }
     dependency_trigger();
@@ -228,11 +251,11 @@ LinearProduct dx_product(const rglru_linear_shape_t *s, const void *dz, const vo
 LinearProduct dw_product(const rglru_linear_shape_t *s, const void *dz, const void *x, void *dweight) {
     return {{dz, s->M, s->N, true}, {x, s->M, s->K, true}, s->N, s->K, s->M, s->io, {nullptr, nullptr, dweight, nullptr, RGLRU_ACT_NONE}};
 }
-bool on_tensor_cores(const rglru_linear_shape_t *s, const LinearProduct &g) { return !(s->flags & RGLRU_FLAG_FORCE_GENERIC) && sm100_linear_wanted(g); }
-size_t product_bytes(const rglru_linear_shape_t *s, const LinearProduct &g) { return on_tensor_cores(s, g) ? sm100_linear_bytes(g) : 0; }
-bool is_few_rows(const rglru_linear_shape_t *s) { return !(s->flags & RGLRU_FLAG_FORCE_GENERIC) && s->M <= FEW_ROWS; }
+bool forced_generic(const rglru_linear_shape_t *s) { return s->flags & RGLRU_FLAG_FORCE_GENERIC; }
+size_t product_bytes(const rglru_linear_shape_t *s, const LinearProduct &g) { return forced_generic(s) ? 0 : sm100_linear_bytes(g); }
+bool is_few_rows(const rglru_linear_shape_t *s) { return !forced_generic(s) && s->M <= FEW_ROWS; }
 cudaError_t run_product(const rglru_linear_shape_t *s, const LinearProduct &g, void *scratch, void *workspace, cudaStream_t st) {
-    if (on_tensor_cores(s, g)) return sm100_linear(g, scratch, (uint32_t *)workspace, st);
+    if (!forced_generic(s)) return sm100_linear(g, scratch, (uint32_t *)workspace, st);
     auto by_row = [](const LinearOperand &o) { return o.turned ? 1ll : o.cols; };
     auto by_k = [](const LinearOperand &o) { return o.turned ? o.cols : 1ll; };
     return generic_gemm(GenericGemm{g.a.p, g.b.p, by_row(g.a), by_k(g.a), by_row(g.b), by_k(g.b), g.M, g.N, g.K, g.e}, g.io, st);
@@ -312,7 +335,7 @@ int32_t rglru_linear_backward(const rglru_linear_shape_t *s, const void *dy, con
     const void *dz = act ? p : dy;
     char *scratch = p + (act ? up256((size_t)s->M * s->N * io_bytes(s->io)) : 0);
     cudaError_t e = cudaSuccess;
-    if (act || dbias) e = linear_dz(s, DzArgs{s->M, s->N, 0, s->activation, dy, preact, act ? p : nullptr, dbias ? part : nullptr}, st);
+    if ((act && (dx || dweight)) || dbias) e = linear_dz(s, DzArgs{s->M, s->N, 0, s->activation, dy, preact, act && (dx || dweight) ? p : nullptr, dbias ? part : nullptr}, st);
     if (e == cudaSuccess && dbias) {
         ReduceJobs jobs{};
         add_reduce_job(jobs, part, dz_blocks(s), s->N, dbias, s->N, nullptr, 0, nullptr, 0);

@@ -3,6 +3,8 @@
 
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "rglru_internal.h"
 #include "sm100_ptx.cuh"
 
@@ -28,8 +30,7 @@ struct LinearProduct {
     int io;
     LinearEpilogue e;
 };
-// Whether the tensor cores serve the product better than the CUDA cores, and the scratch that it takes
-bool sm100_linear_wanted(const LinearProduct &g);
+// The scratch that the product takes
 size_t sm100_linear_bytes(const LinearProduct &g);
 cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status, cudaStream_t st);
 
@@ -40,11 +41,11 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
 constexpr float SQRT_HALF = 0.70710678118654752440f, INV_SQRT_2PI = 0.39894228040143267794f, LOG2_E = 1.44269504088896340736f;
 __device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) { return ptx::fma2(a, b, c); }
 __device__ __forceinline__ float2 both_of(float x) { return make_float2(x, x); }
-// Phi(-|z|) and exp(-z^2 / 2) of two values whose magnitudes a are held at 30
+// Phi(-|z|) and exp(-z^2 / 2) of two values whose magnitudes a are held at 30 (numbers: one reciprocal serves both)
 struct Normal { float2 tail, density; };
 __device__ __forceinline__ Normal normal_tail(float2 a) {
     const float2 d = fma_pair(a, both_of(0.3275911f * SQRT_HALF), both_of(1.0f));
-    const float2 t = make_float2(ptx::rcp_approx(d.x), ptx::rcp_approx(d.y));
+    const float2 t = ptx::mul2(make_float2(d.y, d.x), both_of(ptx::rcp_approx(d.x * d.y)));
     float2 p = fma_pair(t, both_of(0.5f * 1.061405429f), both_of(0.5f * -1.453152027f));
     p = fma_pair(p, t, both_of(0.5f * 1.421413741f));
     p = fma_pair(p, t, both_of(0.5f * -0.284496736f));
@@ -53,13 +54,18 @@ __device__ __forceinline__ Normal normal_tail(float2 a) {
     const float2 e = make_float2(ptx::ex2_approx(x.x), ptx::ex2_approx(x.y));
     return {ptx::mul2(ptx::mul2(p, t), e), e};
 }
-__device__ __forceinline__ float held(float z, float most) { return z > most ? most : z < -most ? -most : z; }   // NaN stays
+__device__ __forceinline__ float held(float z, float most) {   // NaN stays
+    float c;
+    asm("{\n.reg .f32 t;\nmin.NaN.f32 t, %1, %2;\nmax.NaN.f32 %0, t, %3;\n}" : "=f"(c) : "f"(z), "f"(most), "f"(-most));
+    return c;
+}
+__device__ __forceinline__ float2 magnitudes(float2 z) { return make_float2(fminf(fabsf(z.x), 30.0f), fminf(fabsf(z.y), 30.0f)); }   // 30 for NaN
 // for bf16 results
 __device__ __forceinline__ float2 activate_fast(float2 z, int kind) {
     if (kind == RGLRU_ACT_NONE) return z;
     if (kind == RGLRU_ACT_GELU) {
-        const float2 a = make_float2(fabsf(held(z.x, 30.0f)), fabsf(held(z.y, 30.0f)));
-        return fma_pair(make_float2(-a.x, -a.y), normal_tail(a).tail, make_float2(z.x > 0.0f ? z.x : 0.0f, z.y > 0.0f ? z.y : 0.0f));
+        const float2 a = magnitudes(z);
+        return fma_pair(make_float2(-a.x, -a.y), normal_tail(a).tail, make_float2(z.x < 0.0f ? 0.0f : z.x, z.y < 0.0f ? 0.0f : z.y));   // (NaN passes)
     }
     const float2 s = make_float2(ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * z.x)), ptx::rcp_approx(1.0f + ptx::ex2_approx(-LOG2_E * z.y)));
     return make_float2(z.x < -100.0f ? 0.0f : z.x * s.x, z.y < -100.0f ? 0.0f : z.y * s.y);
@@ -67,7 +73,7 @@ __device__ __forceinline__ float2 activate_fast(float2 z, int kind) {
 __device__ __forceinline__ float2 slope_fast(float2 z, int kind) {
     if (kind == RGLRU_ACT_GELU) {
         const float2 c = make_float2(held(z.x, 30.0f), held(z.y, 30.0f));
-        const Normal n = normal_tail(make_float2(fabsf(c.x), fabsf(c.y)));
+        const Normal n = normal_tail(magnitudes(z));
         const float2 phi = make_float2(c.x > 0.0f ? 1.0f - n.tail.x : n.tail.x, c.y > 0.0f ? 1.0f - n.tail.y : n.tail.y);
         return fma_pair(ptx::mul2(c, both_of(INV_SQRT_2PI)), n.density, phi);
     }
@@ -100,19 +106,18 @@ template <bool FAST> __device__ __forceinline__ float activation_slope(float z, 
 }
 
 template <typename IO, int VE> struct LinearVec {
-    static __device__ __forceinline__ void load(const IO *p, float (&f)[VE]) {
+    using Raw = std::conditional_t<VE == 1, IO, uint4>;   // as it lies in memory
+    static __device__ __forceinline__ void unpack(const Raw &v, float (&f)[VE]) {
         if constexpr (VE == 1) {
-            if constexpr (sizeof(IO) == 4) f[0] = *p;
-            else f[0] = __bfloat162float(*p);
+            f[0] = (float)v;
         } else if constexpr (sizeof(IO) == 4) {
-            const float4 v = *(const float4 *)p;
-            f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+            f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
         } else {
-            const uint4 v = *(const uint4 *)p;
             const float2 a = ptx::bf2x(v.x), b = ptx::bf2x(v.y), c = ptx::bf2x(v.z), d = ptx::bf2x(v.w);
             f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
         }
     }
+    static __device__ __forceinline__ void load(const IO *p, float (&f)[VE]) { unpack(*(const Raw *)p, f); }
     static __device__ __forceinline__ void store(IO *p, const float (&f)[VE]) {
         if constexpr (VE == 1) {
             if constexpr (sizeof(IO) == 4) *p = f[0];

@@ -20,7 +20,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int THREADS = 320;              // TMA warp, MMA warp, eight epilogue warps
+constexpr int THREADS = 352;              // a warp for A's copies, one for the products, one for B's copies, eight for the epilogue
 constexpr uint32_t A_BYTES = 128 * 128, RING = 7 * 2 * A_BYTES;   // a CTA's 128 rows of a K block of 64 bf16; all stages
 constexpr int MAX_STAGES = 12;            // a stage is A_BYTES and 64 NT bytes of B: 7 of NT = 256, 12 of NT = 32
 constexpr uint32_t MN_BLOCK = 64 * 128;   // one copy of 64 K rows x 64 values of an operand turned
@@ -184,7 +184,8 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
         return Tile{xy / p.ny * 256, xy % p.ny * p.NT, s * p.per_split, min(p.vblocks, (s + 1) * p.per_split), p.splits > 1 ? u : -1};
     };
 
-    if (warp == 0) {
+    if (warp == 0 || warp == 2) {
+        // (a copy takes its thread some 120 cycles: one thread for both operands would be slower than the products of a narrow tile)
         if (elect_one()) {
             int s = 0;   // stage of the ring, and its turn
             uint32_t turn = 0;
@@ -196,20 +197,16 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
                 for (int v = tl.v0; v < tl.v1; ++v) {
                     ok = mbar_wait_spin(BAR_EMPTY(s), turn ^ 1, spin, abort_flag);
                     if (!ok) break;
-                    if (rank == 0) mbar_expect_tx(BAR_FULL(s), tx);
+                    if (warp == 0 && rank == 0) mbar_expect_tx(BAR_FULL(s), tx);
                     const int prod = p.split_planes ? v / p.kblocks : 0, k0 = (v - prod * p.kblocks) * 64;
                     const int pa = p.split_planes ? PLANE_A[prod] : 0, pb = p.split_planes ? PLANE_B[prod] : 0;
                     const uint32_t a_dst = base + s * stage_bytes, b_dst = a_dst + A_BYTES;
-                    if (p.a_turned) {
-                        tma_load_3d_pair(a_dst, &p.tm_a, ma, k0, pa, BAR_FULL(s));
-                        tma_load_3d_pair(a_dst + MN_BLOCK, &p.tm_a, ma + 64, k0, pa, BAR_FULL(s));
+                    if (warp == 0) {
+                        tma_load_3d_pair(a_dst, &p.tm_a, p.a_turned ? ma : k0, p.a_turned ? k0 : ma, pa, BAR_FULL(s));
+                        if (p.a_turned) tma_load_3d_pair(a_dst + MN_BLOCK, &p.tm_a, ma + 64, k0, pa, BAR_FULL(s));
                     } else {
-                        tma_load_3d_pair(a_dst, &p.tm_a, k0, ma, pa, BAR_FULL(s));
-                    }
-                    if (p.b_turned) {
-                        for (int j = 0; j < brows; j += 64) tma_load_3d_pair(b_dst + j / 64 * MN_BLOCK, &p.tm_b, nb + j, k0, pb, BAR_FULL(s));
-                    } else {
-                        tma_load_3d_pair(b_dst, &p.tm_b, k0, nb, pb, BAR_FULL(s));
+                        tma_load_3d_pair(b_dst, &p.tm_b, p.b_turned ? nb : k0, p.b_turned ? k0 : nb, pb, BAR_FULL(s));
+                        if (p.b_turned && brows > 64) tma_load_3d_pair(b_dst + MN_BLOCK, &p.tm_b, nb + 64, k0, pb, BAR_FULL(s));
                     }
                     if (++s == stages) { s = 0; turn ^= 1; }
                 }
@@ -219,6 +216,9 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
             const uint32_t idesc = instruction(256, p.NT, p.a_turned, p.b_turned);
+            // 16 of K an instruction: 32 bytes along a row, or 16 rows (descriptors count in units of 16 bytes)
+            const uint64_t a0 = p.a_turned ? make_desc_sw128_mn(base, MN_BLOCK) : make_desc_sw128(base), a_step = p.a_turned ? 128 : 2;
+            const uint64_t b0 = p.b_turned ? make_desc_sw128_mn(base + A_BYTES, MN_BLOCK) : make_desc_sw128(base + A_BYTES), b_step = p.b_turned ? 128 : 2;
             int s = 0, it = 0;   // it: accumulators begun
             uint32_t turn = 0;
             for (int t = pair; t < ntiles && ok; t += npairs) {
@@ -229,11 +229,11 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
                     ok = ok && mbar_wait_spin(BAR_FULL(s), turn, spin, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t a = base + s * stage_bytes, b = a + A_BYTES, d = tmem + acc * 256;
+                    const uint64_t at = (uint64_t)s * (stage_bytes / 16), da = a0 + at, db = b0 + at;
+                    const uint32_t d = tmem + acc * 256;
+                    mma_ss2(d, da, db, idesc, within != 0);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)   // 16 of K an instruction: 32 bytes along a row, or 16 rows
-                        mma_ss2(d, p.a_turned ? make_desc_sw128_mn(a + k * 2048, MN_BLOCK) : make_desc_sw128(a + k * 32),
-                                p.b_turned ? make_desc_sw128_mn(b + k * 2048, MN_BLOCK) : make_desc_sw128(b + k * 32), idesc, (within | k) != 0);
+                    for (int k = 1; k < 4; ++k) mma_ss2(d, da + k * a_step, db + k * b_step, idesc, 1);
                     tc_commit2(BAR_EMPTY(s), 3);
                     if (v + 1 == tl.v1 || (DRAIN && within + 1 == DRAIN_BLOCKS)) { tc_commit2(BAR_ACCFULL(acc), 3); ++it; }
                     if (++s == stages) { s = 0; turn ^= 1; }
@@ -242,7 +242,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
             if (!ok) { *abort_flag = 1; atomicExch(p.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;   // tensor-memory lanes 32 q .. + 31, every other 32 columns
+        const int q = warp & 3, half = (warp - 3) >> 2;   // tensor-memory lanes 32 q .. + 31, every other 32 columns
         int it = 0;
         for (int t = pair; t < ntiles && ok; t += npairs) {
             const Tile tl = tile_at(t);
@@ -493,8 +493,6 @@ struct Device {
 } g_device;
 
 }  // namespace
-
-bool sm100_linear_wanted(const LinearProduct &g) { return g.M * g.N >= 1 && g.K >= 1; }
 
 size_t sm100_linear_bytes(const LinearProduct &g) {
     const Plan p = make_plan(g);
