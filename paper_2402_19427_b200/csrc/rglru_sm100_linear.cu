@@ -423,13 +423,13 @@ Plan make_plan(const LinearProduct &g) {
     p.kblocks = (int)((g.K + 63) / 64);
     p.vblocks = p.kblocks * (f32(g) ? PRODUCTS : 1);
     // Whole rounds of pairs take a tile each; the tiles of the last, partly filled round are split along K over all pairs.  The tile width and
-    // the splits are those that take the busiest pair the fewest cycles: a K block costs about 256 + NT of them (copies out of L2 and
-    // products), a tile some 200 more, a split its partial results' way to memory and back and another launch.
+    // the splits are those that take the busiest pair the fewest cycles: a K block costs what its copies out of L2 do (measured: 590
+    // cycles of NT = 256, 470 of 128), a tile some 200 more, a split its partial results' way to memory and back and another launch.
     double best = 0;
     for (int nt : {256, 128, 64, 32}) {
         if ((f32(g) && nt > 128) || (b.turned && nt < 128)) continue;   // registers of the sums; copies 64 values wide
         const long long nx = (M + 255) / 256, ny = (N + nt - 1) / nt, tiles = nx * ny, whole = tiles / PAIRS * PAIRS, rest = tiles - whole;
-        const double block = 256 + nt;
+        const double block = 350 + 0.94 * nt;
         for (int s = 1; s <= 32 && s <= p.vblocks; ++s) {
             const int per = (p.vblocks + s - 1) / s;
             if ((p.vblocks + per - 1) / per != s || (rest == 0 && s > 1)) continue;
