@@ -267,7 +267,8 @@ int32_t rglru_query_status(void *workspace, void *cuda_stream);
  * (rglru_linear*, rglru_linear_attention* below) its projections and a second mixer of the same kind.  The conventions at
  * the top of this file hold: dense row-major device tensors owned by the caller, fp32 per-channel vectors, sums and
  * statistics in fp32, asynchronous on `cuda_stream`, errors as return codes, capturable.  Every kernel waits for the work before it
- * on the stream before it reads or writes global memory.
+ * on the stream before it reads or writes global memory.  A workspace may hold anything when a call starts; calls that may run at the same time need
+ * one each (two captured graphs that are replayed in turn may share one).
  */
 
 /*
@@ -355,6 +356,8 @@ int32_t rglru_linear_backward(const rglru_linear_shape_t *shape, const void *dy,
  * projection's output, and time-major batches need no copy.  Tokens must not overlap one another.
  * Prefill and backward: dk and dv up to 256.  The state and all sums are fp32; bf16 calls round products of q and k, and
  * the state where an output reads it, to bf16 (s_T and ds0 stay as exact as fp32 sums are).
+ * What is no number in q, k or v touches no earlier token, no other head and no other sequence.  In bf16 calls of widths up to 128 an infinity in k
+ * or v counts as NaN: it makes its row (k) or column (v) of the state NaN from its token on.
  */
 typedef struct { int64_t token, batch; } rglru_stride_t;
 typedef struct { rglru_stride_t q, k, v, o, dq, dk, dv; } rglru_linear_attention_strides_t; /* o: also of do */

@@ -218,10 +218,11 @@ template <typename IO, int VE> __global__ void __launch_bounds__(256, 2) linear_
     }
 }
 
-// Rows a block of linear_dz_kernel takes: about eight blocks an SM over the whole call, at least 64 rows (eight a warp)
+// Rows a block of linear_dz_kernel takes: about eight blocks an SM over the whole call, at least 64 rows (eight a warp), at most as many blocks
+// as a grid has along y
 int dz_rows(const rglru_linear_shape_t *s) {
-    const long long cols = (s->N + 255) / 256, want = s->M * cols / (148 * 8);
-    return (int)(want < 64 ? 64 : want > 4096 ? 4096 : (want + 7) / 8 * 8);
+    const long long cols = (s->N + 255) / 256, want = s->M * cols / (148 * 8), most = s->M / 32768 + 8 > 4096 ? s->M / 32768 + 8 : 4096;
+    return (int)(want < 64 ? 64 : want > most ? most / 8 * 8 : (want + 7) / 8 * 8);
 }
 int dz_blocks(const rglru_linear_shape_t *s) { return ceil_div((size_t)s->M, dz_rows(s)); }
 
