@@ -11,7 +11,7 @@ namespace {
 using namespace ptx;
 
 constexpr int MAX_WIDTH = 256;
-constexpr int C = 32, SLICE = 64, GEN_THREADS = 256;   // tokens a chunk, columns of v a block
+constexpr int C = 32, GEN_THREADS = 256;   // tokens a chunk
 
 template <typename IO> __device__ __forceinline__ float at(const void *p, long long i) {
     if constexpr (sizeof(IO) == 4) return ((const float *)p)[i];
@@ -21,130 +21,254 @@ template <typename IO> __device__ __forceinline__ void put(void *p, long long i,
     if constexpr (sizeof(IO) == 4) ((float *)p)[i] = v;
     else ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
 }
+// ---- any type and width: fp32 on the CUDA cores.
+// A block walks chunks of 32 tokens of a (role, sequence, head) for 32 CB columns of v, its part of the state in shared memory.  A chunk is
+//     far = q S,   P = q k^T (decayed, masked; over q's place),   out = P v + decay far,   S <- d^n S + (decayed k)^T v
+// A warp has 32 columns: lane (rg, cg) owns four of them and every fourth row, so that an operand read by 16 bytes serves 16 products and
+// comes without bank conflicts.  Bound by the CUDA cores' instructions (dk = dv = 128: some 16 thousand issue slots of each scheduler a chunk, 15 us of an
+// SM's, 55 % of the slots taken), with two blocks an SM so that one's loads and barriers lie under the other's products: q, k, v, S take half
+// the SM's shared memory to the byte, the powers of the decay lie in the padding of k's rows.  8 x 2048 tokens of 20 heads take 1.5 ms.
+// Long sequences of few heads are cut into equal segments: a first launch leaves the sums of each (STATE_ONLY), and a segment's block starts
+// from the state before it, folded in order (65536 tokens of 16 heads 4.0 ms, in one piece 25 ms).
+struct GenericArgs {
+    MixArgs m;
+    int slices, segments, launched, seg_chunks, rows;   // launched: segments of this launch; rows: of a sum in `local`
+    float *local;                                       // [role][sequence, head][slice][segment][rows][32 CB]
+};
 __host__ __device__ inline int padded_width(int dk) { return (dk + 3) / 4 * 4 + 4; }
-inline size_t generic_smem(int dk) { return sizeof(float) * (2 * C * padded_width(dk) + C * SLICE + (size_t)dk * SLICE + C * (C + 1) + C + 1); }
-
-// One block walks the chunks of a (sequence, head) for 64 columns of v, its part of the state in shared memory.  Everything is fp32.
-template <typename IO> __global__ void __launch_bounds__(GEN_THREADS) generic_mix_kernel(const __grid_constant__ MixArgs a) {
+constexpr int PLD = 36;   // distance of P's rows
+inline size_t generic_smem(int dk, int cb) {
+    const int ld = padded_width(dk), q = C * ld > C * PLD ? C * ld : C * PLD;
+    return sizeof(float) * (size_t)(q + C * ld + C * 32 * cb + (ld - 4) * 32 * cb);
+}
+template <typename IO, int VEC> __device__ __forceinline__ float4 at4(const void *p, long long i) {
+    if constexpr (VEC == 1) {
+        return make_float4(at<IO>(p, i), 0.0f, 0.0f, 0.0f);
+    } else if constexpr (sizeof(IO) == 4) {
+        return *(const float4 *)((const float *)p + i);
+    } else {
+        const uint2 w = *(const uint2 *)((const __nv_bfloat16 *)p + i);
+        const f32x2 a = bf2x(w.x), b = bf2x(w.y);
+        return make_float4(a.x, a.y, b.x, b.y);
+    }
+}
+// VEC: 4 where every width and distance is a multiple of 4
+template <typename IO, int CB, int VEC, bool STATE_ONLY> __global__ void __launch_bounds__(GEN_THREADS, 2) generic_mix_kernel(const __grid_constant__ GenericArgs p) {
+    constexpr int NC = 32 * CB;
     extern __shared__ float4 smem4[];
     dependency_wait();
+    const MixArgs &a = p.m;
     const MixRole &r = a.role[blockIdx.y];
-    const int dk = r.dk, dv = r.dv, ld = padded_width(dk), slices = gridDim.x / (a.B * a.H), c0 = blockIdx.x % slices * SLICE;
-    const int unit = blockIdx.x / slices, h = unit % a.H, b = unit / a.H, tid = threadIdx.x;
+    const int seg = blockIdx.x % p.launched, column = blockIdx.x / p.launched, slice = column % p.slices, unit = column / p.slices;
+    const int dk = r.dk, dv = r.dv, dk4 = (dk + 3) / 4 * 4, ld = dk4 + 4, c0 = slice * NC, h = unit % a.H, b = unit / a.H;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rg = lane >> 3, col = warp % CB * 32 + (lane & 7) * 4, group = warp / CB;
     if (c0 >= dv) return;
-    float *Q = (float *)smem4, *K = Q + C * ld, *V = K + C * ld, *S = V + C * SLICE, *P = S + dk * SLICE, *pw = P + C * (C + 1);
-    const long long mat = (long long)unit * dk * dv;
-    if (tid <= C) pw[tid] = decay_power(a.log_decay[h], (float)tid);
-    for (int i = tid; i < dk * SLICE; i += GEN_THREADS) {
-        const int d = i / SLICE, e = c0 + i % SLICE;
-        S[i] = r.s_in && e < dv ? r.s_in[mat + (r.turned ? (long long)e * dk + d : (long long)d * dv + e)] : 0.0f;
+    float *Q = (float *)smem4, *K = Q + (C * ld > C * PLD ? C * ld : C * PLD), *V = K + C * ld, *S = V + C * NC, *P = Q;
+    const float decay = a.log_decay[h], pw32 = decay_power(decay, 32.0f);
+    auto pw = [&](int n) { return n == 32 ? pw32 : K[n * ld + dk4]; };
+    const int chunks = (a.T + C - 1) / C, first = seg * p.seg_chunks, last = min(chunks, first + p.seg_chunks);
+    const long long mat = (long long)unit * dk * dv, sums = (((long long)blockIdx.y * a.B * a.H + unit) * p.slices + slice) * p.segments;
+    const float before = STATE_ONLY ? 0.0f : decay_power(decay, (float)(p.seg_chunks * C));
+    for (int i = tid; i < dk4 * NC; i += GEN_THREADS) {
+        const int d = i / NC, e = c0 + i % NC;
+        float s = 0.0f;
+        if (!STATE_ONLY) {
+            if (r.s_in && d < dk && e < dv) s = r.s_in[mat + (r.turned ? (long long)e * dk + d : (long long)d * dv + e)];
+            for (int g = 0; g < seg; ++g) s = fmaf(before, s, p.local[(sums + g) * p.rows * NC + i]);
+        }
+        S[i] = s;
     }
-    for (int i = tid; i < 2 * C * ld; i += GEN_THREADS) Q[i] = 0.0f;   // the padding behind dk as well
-    const int ty = tid >> 4, tx = tid & 15;
-    for (int t0 = 0; t0 < a.T; t0 += C) {
-        const int n = min(C, a.T - t0);
+    for (int i = tid; i < C * 4; i += GEN_THREADS) K[i / 4 * ld + dk4 + i % 4] = decay_power(decay, (float)(i / 4));
+    for (int c = first; c < last; ++c) {
+        const int t0 = c * C, n = min(C, a.T - t0);
         __syncthreads();
-        for (int i = tid; i < C * dk; i += GEN_THREADS) {
-            const int j = i / dk, d = i % dk, t = r.reverse ? a.T - 1 - (t0 + j) : t0 + j;
-            const bool in = j < n;
-            Q[j * ld + d] = in ? at<IO>(r.q.p, b * r.q.batch + t * r.q.token + (long long)h * dk + d) : 0.0f;
-            K[j * ld + d] = in ? at<IO>(r.k.p, b * r.k.batch + t * r.k.token + (long long)h * dk + d) : 0.0f;
-        }
-        for (int i = tid; i < C * SLICE; i += GEN_THREADS) {
-            const int j = i / SLICE, e = c0 + i % SLICE, t = r.reverse ? a.T - 1 - (t0 + j) : t0 + j;
-            V[i] = j < n && e < dv ? at<IO>(r.v.p, b * r.v.batch + t * r.v.token + (long long)h * dv + e) : 0.0f;
-        }
-        __syncthreads();
-        {   // P[i][j] = sp d^(i-j) q_i k_j for j <= i
-            float p[2][2] = {};
-            if (tx <= ty)
-                for (int d = 0; d < dk; d += 4) {
-                    const float4 q0 = *(const float4 *)&Q[(2 * ty) * ld + d], q1 = *(const float4 *)&Q[(2 * ty + 1) * ld + d];
-                    const float4 k0 = *(const float4 *)&K[(2 * tx) * ld + d], k1 = *(const float4 *)&K[(2 * tx + 1) * ld + d];
-                    p[0][0] += q0.x * k0.x + q0.y * k0.y + q0.z * k0.z + q0.w * k0.w;
-                    p[0][1] += q0.x * k1.x + q0.y * k1.y + q0.z * k1.z + q0.w * k1.w;
-                    p[1][0] += q1.x * k0.x + q1.y * k0.y + q1.z * k0.z + q1.w * k0.w;
-                    p[1][1] += q1.x * k1.x + q1.y * k1.y + q1.z * k1.z + q1.w * k1.w;
-                }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const int i = 2 * ty + u, j = 2 * tx + w;
-                    P[i * (C + 1) + j] = j <= i ? p[u][w] * (r.sp * pw[i - j]) : 0.0f;
-                }
-        }
-        __syncthreads();
-        {   // outputs of rows 2 ty, 2 ty + 1, four columns
-            float near[2][4] = {}, far[2][4] = {};
-            for (int d = 0; d < dk; ++d) {
-                const float4 s = *(const float4 *)&S[d * SLICE + tx * 4];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const float q = Q[(2 * ty + u) * ld + d];
-                    far[u][0] = fmaf(q, s.x, far[u][0]); far[u][1] = fmaf(q, s.y, far[u][1]);
-                    far[u][2] = fmaf(q, s.z, far[u][2]); far[u][3] = fmaf(q, s.w, far[u][3]);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                for (int j = 0; j <= 2 * ty + u; ++j) {   // later tokens are not touched: what they hold may be no number
-                    const float4 v = *(const float4 *)&V[j * SLICE + tx * 4];
-                    const float p = P[(2 * ty + u) * (C + 1) + j];
-                    near[u][0] = fmaf(p, v.x, near[u][0]); near[u][1] = fmaf(p, v.y, near[u][1]);
-                    near[u][2] = fmaf(p, v.z, near[u][2]); near[u][3] = fmaf(p, v.w, near[u][3]);
-                }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int i = 2 * ty + u, t = r.reverse ? a.T - 1 - (t0 + i) : t0 + i;
-                if (i >= n) continue;
-                const float w = r.si * pw[i + r.first];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c0 + tx * 4 + e < dv) put<IO>(r.o.p, b * r.o.batch + t * r.o.token + (long long)h * dv + c0 + tx * 4 + e, fmaf(w, far[u][e], near[u][e]));
-            }
-        }
-        __syncthreads();
-        for (int d0 = ty; d0 < dk; d0 += 64) {   // state rows d0, d0 + 16, d0 + 32, d0 + 48, four columns
-            float s[4][4] = {};
-            for (int j = 0; j < n; ++j) {
-                const float4 v = *(const float4 *)&V[j * SLICE + tx * 4];
-                const float w = r.su * pw[n - j - r.first];
+        auto load = [&](const MixTensor &t, float *to, int width, int from, int wide, int distance) {   // columns from, from + 1, .. of 32 tokens, zeros behind them
+            for (int d = lane * VEC; d < wide; d += 32 * VEC) {
+                float4 x[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    const float k = d0 + 16 * u < dk ? w * K[j * ld + d0 + 16 * u] : 0.0f;
-                    s[u][0] = fmaf(k, v.x, s[u][0]); s[u][1] = fmaf(k, v.y, s[u][1]); s[u][2] = fmaf(k, v.z, s[u][2]); s[u][3] = fmaf(k, v.w, s[u][3]);
+                    const int j = warp + 8 * u, token = r.reverse ? a.T - 1 - (t0 + j) : t0 + j;
+                    x[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (j < n && from + d < width) x[u] = at4<IO, VEC>(t.p, b * t.batch + token * t.token + (long long)h * width + from + d);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float *at_row = to + (warp + 8 * u) * distance + d;
+                    if constexpr (VEC == 4) *(float4 *)at_row = x[u];
+                    else *at_row = x[u].x;
+                }
+            }
+        };
+        if (!STATE_ONLY) load(r.q, Q, dk, 0, dk4, ld);
+        load(r.k, K, dk, 0, dk4, ld);
+        load(r.v, V, dv, c0, NC, NC);
+        __syncthreads();
+        if (!STATE_ONLY) {
+            const int row = group * 4 * CB + rg;   // and every fourth from there on
+            float far[CB][4] = {};
+#pragma unroll 2
+            for (int d = 0; d < dk4; d += 4) {
+                float4 s[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = *(const float4 *)&S[(d + e) * NC + col];
+#pragma unroll
+                for (int u = 0; u < CB; ++u) {
+                    const float4 q = *(const float4 *)&Q[(row + 4 * u) * ld + d];
+                    const float x[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        far[u][0] = fmaf(x[e], s[e].x, far[u][0]); far[u][1] = fmaf(x[e], s[e].y, far[u][1]);
+                        far[u][2] = fmaf(x[e], s[e].z, far[u][2]); far[u][3] = fmaf(x[e], s[e].w, far[u][3]);
+                    }
+                }
+            }
+            float x[4] = {};   // rows 4 warp .. + 3 of P, column lane
+            for (int d = 0; d < dk4; d += 4) {
+                const float4 k = *(const float4 *)&K[lane * ld + d];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float4 q = *(const float4 *)&Q[(4 * warp + u) * ld + d];
+                    x[u] = fmaf(q.x, k.x, x[u]); x[u] = fmaf(q.y, k.y, x[u]); x[u] = fmaf(q.z, k.z, x[u]); x[u] = fmaf(q.w, k.w, x[u]);
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = 4 * warp + u;
+                P[i * PLD + lane] = lane <= i ? x[u] * (r.sp * pw(i - lane)) : 0.0f;
+            }
+            __syncthreads();
+            float near[CB][4] = {};
+            for (int j = 0; j < group * 4 * CB + 4 * CB; j += 4) {
+                float4 v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = *(const float4 *)&V[(j + e) * NC + col];
+#pragma unroll
+                for (int u = 0; u < CB; ++u) {
+                    const float4 w = *(const float4 *)&P[(row + 4 * u) * PLD + j];
+                    const float y[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (j + e > row + 4 * u) continue;   // later tokens are not touched: what they hold may be no number
+                        near[u][0] = fmaf(y[e], v[e].x, near[u][0]); near[u][1] = fmaf(y[e], v[e].y, near[u][1]);
+                        near[u][2] = fmaf(y[e], v[e].z, near[u][2]); near[u][3] = fmaf(y[e], v[e].w, near[u][3]);
+                    }
                 }
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (d0 + 16 * u >= dk) continue;
-                float4 *p = (float4 *)&S[(d0 + 16 * u) * SLICE + tx * 4];
-                const float4 o = *p;
-                *p = make_float4(fmaf(pw[n], o.x, s[u][0]), fmaf(pw[n], o.y, s[u][1]), fmaf(pw[n], o.z, s[u][2]), fmaf(pw[n], o.w, s[u][3]));
+            for (int u = 0; u < CB; ++u) {
+                const int i = row + 4 * u, token = r.reverse ? a.T - 1 - (t0 + i) : t0 + i;
+                if (i >= n) continue;
+                const float w = r.si * pw(i + r.first);
+                const long long o = b * r.o.batch + token * r.o.token + (long long)h * dv + c0 + col;
+                const float y[4] = {fmaf(w, far[u][0], near[u][0]), fmaf(w, far[u][1], near[u][1]), fmaf(w, far[u][2], near[u][2]), fmaf(w, far[u][3], near[u][3])};
+                if (VEC == 4 && sizeof(IO) == 4 && c0 + col < dv) {
+                    *(float4 *)((float *)r.o.p + o) = make_float4(y[0], y[1], y[2], y[3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c0 + col + e < dv) put<IO>(r.o.p, o + e, y[e]);
+                }
+            }
+        }
+        if (!STATE_ONLY && c + 1 == last && !(last == chunks && r.s_out)) break;   // nobody reads the state behind
+        const float f = pw(n);
+        for (int tile = 0; tile < dk4; tile += 128) {   // rows tile + 16 CB group + 16 i + 4 rg + e
+            const int row = tile + group * 16 * CB + rg * 4;
+            f32x2 sum[CB][2][4] = {};   // pairs of rows, four columns
+            for (int j = 0; j < n; ++j) {
+                const float4 v = *(const float4 *)&V[j * NC + col];
+                const float w = r.su * pw(n - j - r.first);
+                const f32x2 x[4] = {pack2(w * v.x, w * v.x), pack2(w * v.y, w * v.y), pack2(w * v.z, w * v.z), pack2(w * v.w, w * v.w)};
+#pragma unroll
+                for (int i = 0; i < CB; ++i) {
+                    if (row + 16 * i >= dk4) continue;
+                    const float4 k = *(const float4 *)&K[j * ld + row + 16 * i];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sum[i][0][e] = fma2(pack2(k.x, k.y), x[e], sum[i][0][e]);
+                        sum[i][1][e] = fma2(pack2(k.z, k.w), x[e], sum[i][1][e]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < CB; ++i) {
+                if (row + 16 * i >= dk4) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float4 *at_row = (float4 *)&S[(row + 16 * i + e) * NC + col];
+                    const float4 o = *at_row;
+                    const f32x2 *z = sum[i][e / 2];
+                    *at_row = e % 2 ? make_float4(fmaf(f, o.x, z[0].y), fmaf(f, o.y, z[1].y), fmaf(f, o.z, z[2].y), fmaf(f, o.w, z[3].y))
+                                    : make_float4(fmaf(f, o.x, z[0].x), fmaf(f, o.y, z[1].x), fmaf(f, o.z, z[2].x), fmaf(f, o.w, z[3].x));
+                }
             }
         }
     }
     __syncthreads();
-    if (r.s_out)
-        for (int i = tid; i < dk * SLICE; i += GEN_THREADS) {
-            const int d = i / SLICE, e = c0 + i % SLICE;
+    if (STATE_ONLY) {
+        for (int i = tid; i < dk4 * NC; i += GEN_THREADS) p.local[(sums + seg) * p.rows * NC + i] = S[i];
+    } else if (r.s_out && last == chunks) {
+        for (int i = tid; i < dk * NC; i += GEN_THREADS) {
+            const int d = i / NC, e = c0 + i % NC;
             if (e < dv) r.s_out[mat + (long long)d * dv + e] = S[i];
         }
+    }
     dependency_trigger();
 }
 
-cudaError_t generic_mix(const MixArgs &a, int io, cudaStream_t st) {
+// What a call on the CUDA cores takes: blocks of 64 columns where no role has more or blocks of 128, cut, would still leave half the SMs idle; segments, as many as make two blocks an SM but no shorter
+// than eight chunks (a segment's sums cost a third of its walk again)
+struct GenericPlan {
+    int cb, slices, segments, seg_chunks, rows;
+    size_t local_bytes;
+};
+GenericPlan generic_plan(int roles, int B, int T, int H, int dk, int dv) {   // dk, dv: the largest of all roles
+    GenericPlan p{};
+    const long long units = (long long)roles * B * H, chunks = (T + C - 1) / C, most = chunks < 16 ? 1 : chunks / 8;
+    p.cb = dv <= 64 || units * ((dv + 127) / 128) * most <= 74 ? 2 : 4;
+    p.slices = (dv + 32 * p.cb - 1) / (32 * p.cb);
+    p.rows = (dk + 3) / 4 * 4;
+    const long long blocks = units * p.slices;
+    long long want = 296 / blocks;
+    if (want > most) want = most;
+    p.segments = want < 2 ? 1 : (int)want;
+    p.seg_chunks = (int)((chunks + p.segments - 1) / p.segments);
+    p.segments = (int)((chunks + p.seg_chunks - 1) / p.seg_chunks);
+    p.local_bytes = p.segments == 1 ? 0 : (size_t)blocks * p.segments * p.rows * 32 * p.cb * sizeof(float);
+    return p;
+}
+template <typename IO, int CB, int VEC> cudaError_t run_generic(const GenericPlan &plan, GenericArgs &p, size_t smem, size_t most, cudaStream_t st) {
+    static PerDeviceOptIn opt, opt_state;
+    const long long columns = (long long)p.m.B * p.m.H * plan.slices;
+    if (columns * plan.segments > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+    cudaError_t e = opt.ensure(generic_mix_kernel<IO, CB, VEC, false>, (int)most);
+    if (e == cudaSuccess && plan.segments > 1) {
+        e = opt_state.ensure(generic_mix_kernel<IO, CB, VEC, true>, (int)most);
+        p.launched = plan.segments - 1;   // nothing comes behind the last one
+        if (e == cudaSuccess) e = launch_dependent(generic_mix_kernel<IO, CB, VEC, true>, dim3((unsigned)(columns * p.launched), p.m.roles), dim3(GEN_THREADS), smem, st, p);
+    }
+    p.launched = plan.segments;
+    if (e == cudaSuccess) e = launch_dependent(generic_mix_kernel<IO, CB, VEC, false>, dim3((unsigned)(columns * p.launched), p.m.roles), dim3(GEN_THREADS), smem, st, p);
+    return e;
+}
+cudaError_t generic_mix(const MixArgs &a, int io, float *local, cudaStream_t st) {
     int dk = 0, dv = 0;
-    for (int i = 0; i < a.roles; ++i) { dk = a.role[i].dk > dk ? a.role[i].dk : dk; dv = a.role[i].dv > dv ? a.role[i].dv : dv; }
-    const long long blocks = (long long)a.B * a.H * ((dv + SLICE - 1) / SLICE);
-    if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks, a.roles);
-    static PerDeviceOptIn opt_f32, opt_bf16;
-    const size_t most = generic_smem(MAX_WIDTH);
-    cudaError_t e = io == RGLRU_F32 ? opt_f32.ensure(generic_mix_kernel<float>, (int)most) : opt_bf16.ensure(generic_mix_kernel<__nv_bfloat16>, (int)most);
-    if (e != cudaSuccess) return e;
-    return launch_dependent(io == RGLRU_F32 ? generic_mix_kernel<float> : generic_mix_kernel<__nv_bfloat16>, grid, dim3(GEN_THREADS), generic_smem(dk), st, a);
+    bool vec = true;
+    for (int i = 0; i < a.roles; ++i) {
+        const MixRole &r = a.role[i];
+        dk = r.dk > dk ? r.dk : dk; dv = r.dv > dv ? r.dv : dv;
+        vec = vec && r.dk % 4 == 0 && r.dv % 4 == 0;
+        for (const MixTensor *t : {&r.q, &r.k, &r.v, &r.o}) vec = vec && (a.T == 1 || t->token % 4 == 0) && (a.B == 1 || t->batch % 4 == 0);
+    }
+    const GenericPlan plan = generic_plan(a.roles, a.B, a.T, a.H, dk, dv);
+    GenericArgs p{a, plan.slices, plan.segments, 0, plan.seg_chunks, plan.rows, local};
+    const size_t smem = generic_smem(dk, plan.cb), most = generic_smem(MAX_WIDTH, plan.cb);
+#define RGLRU_GENERIC(IO) \
+    (plan.cb == 2 ? (vec ? run_generic<IO, 2, 4>(plan, p, smem, most, st) : run_generic<IO, 2, 1>(plan, p, smem, most, st)) \
+                  : (vec ? run_generic<IO, 4, 4>(plan, p, smem, most, st) : run_generic<IO, 4, 1>(plan, p, smem, most, st)))
+    return io == RGLRU_F32 ? RGLRU_GENERIC(float) : RGLRU_GENERIC(__nv_bfloat16);
+#undef RGLRU_GENERIC
 }
 
 // ---- decode step: s = d s + k v^T, o = scale q s.  Bound by the state, read and written once.  A thread owns VE columns of every 256 / LPR-th
@@ -235,17 +359,23 @@ size_t state_bytes(const rglru_linear_attention_shape_t *s) { return (size_t)s->
 bool may_use_tensor_cores(const rglru_linear_attention_shape_t *s) {
     return !(s->flags & RGLRU_FLAG_FORCE_GENERIC) && s->io == RGLRU_BF16 && s->dk <= 128 && s->dv <= 128 && s->dk % 8 == 0 && s->dv % 8 == 0;
 }
+// Sums of stretches of cut sequences, by either kernel: a call's strides decide between them, its size must do for both
+size_t sums_bytes(const rglru_linear_attention_shape_t *s, int roles) {
+    const int wide = s->dk > s->dv ? s->dk : s->dv;
+    const size_t generic = roles == 1 ? generic_plan(1, s->B, s->T, s->H, s->dk, s->dv).local_bytes : generic_plan(roles, s->B, s->T, s->H, wide, wide).local_bytes;
+    const size_t tensor = may_use_tensor_cores(s) ? sm100_mix_bytes(roles, s->B, s->T, s->H) : 0;
+    return generic > tensor ? generic : tensor;
+}
 cudaError_t run_mix(const rglru_linear_attention_shape_t *s, MixArgs &a, void *workspace, cudaStream_t st) {
-    if (!may_use_tensor_cores(s) || !sm100_mix_supported(a, s->io)) return generic_mix(a, s->io, st);
     char *scratch = (char *)workspace + WS_HEADER_BYTES;
-    const size_t sums = sm100_mix_bytes(a.roles, s->B, s->T, s->H);
+    const size_t sums = sums_bytes(s, a.roles);
     if (sums && a.role[0].s_in && a.role[0].s_in == a.role[0].s_out) {   // blocks that share a sequence all read its s0
         float *copy = (float *)(scratch + up256(sums));
         const cudaError_t e = cudaMemcpyAsync(copy, a.role[0].s_in, state_bytes(s), cudaMemcpyDeviceToDevice, st);
         if (e != cudaSuccess) return e;
         a.role[0].s_in = copy;
     }
-    return sm100_mix(a, scratch, st);
+    return may_use_tensor_cores(s) && sm100_mix_supported(a, s->io) ? sm100_mix(a, scratch, st) : generic_mix(a, s->io, (float *)scratch, st);
 }
 
 }  // namespace
@@ -261,7 +391,7 @@ size_t rglru_linear_attention_workspace_bytes(const rglru_linear_attention_shape
     // the copy of s0 is for a call that overwrites it (s_T == s0) while blocks read it
     const int roles = op == RGLRU_OP_PREFILL ? 1 : 3;
     size_t bytes = WS_HEADER_BYTES;
-    const size_t sums = may_use_tensor_cores(s) ? sm100_mix_bytes(roles, s->B, s->T, s->H) : 0;
+    const size_t sums = sums_bytes(s, roles);
     if (sums) bytes += up256(sums) + (roles == 1 ? up256(state_bytes(s)) : 0);
     return bytes;
 }

@@ -206,3 +206,23 @@ def test_graph_replay_and_two_streams():
     graph.replay(); graph.replay(); torch.cuda.synchronize()
     for g in got:
         assert all(torch.equal(a, b) for a, b in zip(g, ref))
+
+
+@pytest.mark.parametrize("io,B,T,H,dk,dv", [("f32", 1, 1100, 2, 64, 128), ("f32", 2, 700, 3, 33, 200), ("bf16", 1, 19300, 2, 128, 128), ("bf16", 1, 900, 1, 136, 256)])
+def test_cut_sequences_whose_state_is_updated_in_place(io, B, T, H, dk, dv):
+    """Sequences long enough to be shared by several blocks, all of which start from s0: it may be where s_T goes"""
+    from paper_2402_19427_b200 import binding
+    t = make(B, T, H, dk, dv, io)
+    o, s_T = binding.linear_attention_prefill(t["q"], t["k"], t["v"], t["ld"], s0=t["s0"])
+    s = t["s0"].clone()
+    o2, _ = binding.linear_attention_prefill(t["q"], t["k"], t["v"], t["ld"], s0=s, s_T=s)
+    assert torch.equal(o, o2) and torch.equal(s, s_T)
+    # the last tokens, and the state, against the walk over those tokens alone from the state before them
+    cut = T - 150
+    _, before = binding.linear_attention_prefill(*(t[n][:, :cut].contiguous() for n in "qkv"), t["ld"], s0=t["s0"])
+    tail = dict(t, **{n: t[n][:, cut:].contiguous() for n in "qkv"}, s0=before)
+    orr, sr, om, sm = bo.attention(tail["q"], tail["k"], tail["v"], t["ld"], before, dk ** -0.5)
+    # both states have come by their own cuts: each is off by fp32 sums of what lies in it, a few half steps of its magnitude a chunk
+    off = 2 * bo.state_bound(sm, T)
+    bo.assert_within("s_T", s_T, sr, off)
+    bo.assert_within("o", o[:, cut:], orr, 2 * bo.attention_bound(om, orr, DT[io], T) + bo.U32 * (512 + T / 8) * om)
