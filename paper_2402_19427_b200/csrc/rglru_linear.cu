@@ -198,8 +198,15 @@ template <typename IO, int VE> __global__ void __launch_bounds__(256, 2) linear_
                     }
                     if (a.dz) Vec::store((IO *)a.dz + (now + 8 * u) * a.N + c, g);
                 }
+                if constexpr (VE > 1) {
 #pragma unroll
-                for (int e = 0; e < VE; ++e) s[e] += g[e];
+                    for (int e = 0; e < VE; e += 2) {
+                        const float2 t = fma_pair(make_float2(g[e], g[e + 1]), both_of(1.0f), make_float2(s[e], s[e + 1]));
+                        s[e] = t.x; s[e + 1] = t.y;
+                    }
+                } else {
+                    s[0] += g[0];
+                }
             }
         }
     }
