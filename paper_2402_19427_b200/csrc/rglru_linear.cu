@@ -80,56 +80,71 @@ template <typename IO> __global__ void __launch_bounds__(256) generic_linear_ker
     dependency_trigger();
 }
 
-// The forward of few rows (tokens): bound by reading the weights once.  A warp takes two outputs; its lanes read 16 bytes of each weight row side by
-// side, and the same columns of up to MT rows of x out of the first-level cache.  Tensor cores would need the weights in shared memory
-// first, the tokens padded and K split over the SMs: 11.4 us for one token of 2560 x 2560.
+// The forward of few rows (tokens): bound by reading the weights once.  A block takes four outputs and its warps share K, so that even a few
+// hundred outputs fill the SMs; a lane reads 16 bytes of each of the four weight rows and, out of the first-level cache, of each row of x.
+// Tensor cores would need the weights in shared memory first, the tokens padded and K split over the SMs by a launch of its own.
+constexpr int FEW_OUT = 4;
 template <typename IO, int VE, int MT> __global__ void __launch_bounds__(256) few_rows_kernel(GenericGemm g) {
+    __shared__ float red[8][FEW_OUT * MT];
+    using Vec = LinearVec<IO, VE>;
+    constexpr int PAIRS = VE > 1 ? VE / 2 : 1;
     dependency_wait();
-    const int lane = threadIdx.x & 31;
-    const long long n0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * 2;
-    if (n0 < g.N) {
-        const IO *w0 = (const IO *)g.b + n0 * g.K, *w1 = n0 + 1 < g.N ? w0 + g.K : w0;
-        float acc[2][MT] = {};
-#pragma unroll 4
-        for (long long k = lane * VE; k < g.K; k += 32 * VE) {
-            float a[VE], b[VE];
-            LinearVec<IO, VE>::load(w0 + k, a);
-            LinearVec<IO, VE>::load(w1 + k, b);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long n0 = (long long)blockIdx.x * FEW_OUT;
+    float2 acc[FEW_OUT][MT] = {};   // even and odd columns
+    auto pairs = [](const float (&f)[VE], float2 (&p)[PAIRS]) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                if (m >= g.M) break;
-                float x[VE];
-                LinearVec<IO, VE>::load((const IO *)g.a + m * g.K + k, x);
+        for (int e = 0; e < PAIRS; ++e) p[e] = make_float2(f[VE > 1 ? 2 * e : 0], VE > 1 ? f[2 * e + 1] : 0.0f);
+    };
+#pragma unroll 2
+    for (long long k = (long long)threadIdx.x * VE; k < g.K; k += 256 * VE) {
+        float2 w[FEW_OUT][PAIRS];
 #pragma unroll
-                for (int e = 0; e < VE; ++e) { acc[0][m] = fmaf(a[e], x[e], acc[0][m]); acc[1][m] = fmaf(b[e], x[e], acc[1][m]); }
-            }
+        for (int i = 0; i < FEW_OUT; ++i) {
+            float f[VE];
+            Vec::load((const IO *)g.b + (n0 + i < g.N ? n0 + i : n0) * g.K + k, f);
+            pairs(f, w[i]);
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
+            if (m >= g.M) break;
+            float f[VE];
+            float2 x[PAIRS];
+            Vec::load((const IO *)g.a + m * g.K + k, f);
+            pairs(f, x);
 #pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                acc[0][m] += __shfl_xor_sync(0xffffffffu, acc[0][m], o);
-                acc[1][m] += __shfl_xor_sync(0xffffffffu, acc[1][m], o);
-            }
-        }
-        // lane (2 m + i) finishes output i of row m
-        float z = 0.0f;
+            for (int i = 0; i < FEW_OUT; ++i)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) z = lane == 2 * m ? acc[0][m] : lane == 2 * m + 1 ? acc[1][m] : z;
-        const long long m = lane >> 1, n = n0 + (lane & 1);
-        if (m < g.M && m < MT && n < g.N) {
-            const LinearEpilogue &e = g.e;
-            const long long o = m * g.N + n;
-            z += e.bias ? e.bias[n] : 0.0f;
-            if (e.preact) put<IO>(e.preact, o, z);
-            put<IO>(e.y, o, activate<sizeof(IO) == 2>(z, e.activation) + (e.residual ? at<IO>(e.residual, o) : 0.0f));
+                for (int e = 0; e < PAIRS; ++e) acc[i][m] = fma_pair(w[i][e], x[e], acc[i][m]);
         }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < FEW_OUT; ++i) {
+            float z = acc[i][m].x + acc[i][m].y;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            if (lane == 0) red[warp][m * FEW_OUT + i] = z;
+        }
+    __syncthreads();
+    const int t = threadIdx.x;
+    const long long m = t / FEW_OUT, n = n0 + t % FEW_OUT;
+    if (t < FEW_OUT * MT && m < g.M && n < g.N) {
+        const LinearEpilogue &e = g.e;
+        const long long o = m * g.N + n;
+        float z = red[0][t];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) z += red[i][t];
+        z += e.bias ? e.bias[n] : 0.0f;
+        if (e.preact) put<IO>(e.preact, o, z);
+        put<IO>(e.y, o, activate<sizeof(IO) == 2>(z, e.activation) + (e.residual ? at<IO>(e.residual, o) : 0.0f));
     }
     dependency_trigger();
 }
 constexpr int FEW_ROWS = 8;
 template <typename IO, int VE> cudaError_t few_rows(const GenericGemm &g, cudaStream_t st) {
-    const dim3 grid((unsigned)((g.N + 15) / 16));
+    const dim3 grid((unsigned)((g.N + FEW_OUT - 1) / FEW_OUT));
     return launch_dependent(g.M == 1 ? few_rows_kernel<IO, VE, 1> : g.M == 2 ? few_rows_kernel<IO, VE, 2> : g.M <= 4 ? few_rows_kernel<IO, VE, 4> : few_rows_kernel<IO, VE, 8>,
                             grid, dim3(256), 0, st, g);
 }
@@ -138,7 +153,8 @@ template <typename IO> cudaError_t few_rows(const GenericGemm &g, cudaStream_t s
     return g.K % MOST == 0 ? few_rows<IO, MOST>(g, st) : few_rows<IO, 1>(g, st);
 }
 
-// dz = dy act'(z) in the io type, and the sums of the unrounded dz over a block's rows.  A thread owns VE columns and walks rows.
+// dz = dy act'(z) in the io type, and the sums of the unrounded dz over a block's rows.  A thread owns VE columns and walks rows.  16384 x 2560 with
+// GeLU: 47 us for 252 MB, bound by the slope's instructions (72 % of the issue slots); the sums alone 19 us for 84 MB.
 struct DzArgs {
     long long M;
     int N, rows;              // rows a block
@@ -261,7 +277,12 @@ LinearProduct dw_product(const rglru_linear_shape_t *s, const void *dz, const vo
 }
 bool forced_generic(const rglru_linear_shape_t *s) { return s->flags & RGLRU_FLAG_FORCE_GENERIC; }
 size_t product_bytes(const rglru_linear_shape_t *s, const LinearProduct &g) { return forced_generic(s) ? 0 : sm100_linear_bytes(g); }
-bool is_few_rows(const rglru_linear_shape_t *s) { return !forced_generic(s) && s->M <= FEW_ROWS; }
+// Up to eight rows of fp32 (8 x 2560 x 2560: 16 us, on the tensor cores 31), of bf16 while the products are few beside the weights' bytes: one row always (2560 x
+// 2560 5.0 and 8.3 us), more up to 2^25 products (4 x 2560 x 2560 9.9 and 10.2, 6 rows 17 and 10; 8 x 512 x 1024 4.8 and 6.6)
+bool is_few_rows(const rglru_linear_shape_t *s) {
+    if (forced_generic(s) || s->M > FEW_ROWS) return false;
+    return s->io == RGLRU_F32 || s->M == 1 || s->M * s->K * (long long)s->N <= 1 << 25;
+}
 cudaError_t run_product(const rglru_linear_shape_t *s, const LinearProduct &g, void *scratch, void *workspace, cudaStream_t st) {
     if (!forced_generic(s)) return sm100_linear(g, scratch, (uint32_t *)workspace, st);
     auto by_row = [](const LinearOperand &o) { return o.turned ? 1ll : o.cols; };
