@@ -27,6 +27,7 @@ constexpr int THREADS = 352;              // a warp for A's copies, one for the 
 constexpr uint32_t A_BYTES = 128 * 128, RING = 7 * 2 * A_BYTES;   // a CTA's 128 rows of a K block of 64 bf16; all stages
 constexpr int MAX_STAGES = 12;            // a stage is A_BYTES and 64 NT bytes of B: 7 of NT = 256, 12 of NT = 32
 constexpr uint32_t MN_BLOCK = 64 * 128;   // one copy of 64 K rows x 64 values of an operand turned
+constexpr uint32_t TURN = 2 * A_BYTES;   // the ring's last bytes where rows start at any byte: 4 KB for each of the epilogue's warps to turn results in
 constexpr uint32_t SMEM_BAR = RING;
 constexpr uint32_t SMEM_TOTAL = SMEM_BAR + (2 * MAX_STAGES + 4) * 8 + 16, SMEM_ALLOC = SMEM_TOTAL + 1024;
 constexpr int PAIRS = 74;                 // the plan, and with it the workspace, does not depend on the device
@@ -73,7 +74,7 @@ template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs
 #pragma unroll
         for (int j = 0; j < 8; ++j) *(float4 *)(dst + 4 * j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
     };
-    if (!p.wide || n0 + 32 > p.N) {
+    if (n0 + 32 > p.N) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             if (n0 + j >= p.N) continue;
@@ -130,6 +131,20 @@ template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs
         }
     }
     store(e.y);
+}
+// The warp's 32 x 32 results where rows start at any byte: turned in shared memory, so that lanes write side by side (a thread's row in pieces of one
+// value took 100 us where this takes 31: 4097 x 1001 to 1531)
+template <typename IO> __device__ __forceinline__ void finish_turned(const GemmArgs &p, long long m0, int n0, int lane, const float *v, float *turn) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 32; ++j) turn[lane * 32 + (j ^ lane)] = v[j];
+    __syncwarp();
+    const int n = n0 + lane;
+    if (n >= p.N) return;
+    const float b = p.e.bias ? p.e.bias[n] : 0.0f;
+    const int rows = (int)min(32ll, p.M - m0);
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) finish_one<IO>(p.e, (m0 + i) * p.out_m + n, turn[i * 32 + (lane ^ i)] + b);
 }
 // 32 results of row m where neighbouring rows are neighbours in memory (tokens along N): lanes write side by side
 template <typename IO> __device__ __forceinline__ void finish_column(const GemmArgs &p, long long m, int n0, const float *v) {
@@ -252,7 +267,12 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
             const long long m = tl.m + (long long)rank * 128 + q * 32 + lane;
             const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
             auto finish = [&](int n0, float *v) {
-                if (m >= p.M || n0 >= p.N) return;
+                if (n0 >= p.N) return;
+                if (tl.part < 0 && p.out_n == 1 && !p.wide) {
+                    finish_turned<IO>(p, m - lane, n0, lane, v, (float *)(smem + RING - TURN) + (warp - 3) * 1024);
+                    return;
+                }
+                if (m >= p.M) return;
                 if (tl.part >= 0) {   // partial sums: whole tiles, in the order that the results have
                     const int row = (int)(m - tl.m), col = n0 - tl.n;
                     float *to = p.part + (size_t)tl.part * 256 * p.NT;
@@ -514,7 +534,6 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
     if ((e = place(ob, g.io, p.pack_b, at + p.a_bytes, p.NT / 2, &a.tm_b, st)) != cudaSuccess) return e;
     a.a_turned = oa.turned; a.b_turned = ob.turned; a.split_planes = f32(g);
     a.M = (int)(p.swapped ? g.N : g.M); a.N = (int)(p.swapped ? g.M : g.N);
-    a.stages = (int)(RING / (A_BYTES + (uint32_t)p.NT * 64u));
     a.NT = p.NT; a.nx = p.nx; a.ny = p.ny;
     a.kblocks = p.kblocks; a.vblocks = p.vblocks; a.whole = p.whole; a.splits = p.splits; a.per_split = p.per_split;
     a.out_m = p.swapped ? 1 : g.N; a.out_n = p.swapped ? g.N : 1;
@@ -522,6 +541,7 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
     a.part = (float *)(at + p.a_bytes + p.b_bytes);
     const int per16 = 16 / (int)io_bytes(g.io);
     a.wide = g.N % per16 != 0 ? 0 : g.N % (2 * per16) == 0 && aligned(g.e.y, 32) && aligned(g.e.preact, 32) ? 32 : 16;
+    a.stages = (int)((a.out_n == 1 && !a.wide ? RING - TURN : RING) / (A_BYTES + (uint32_t)p.NT * 64u));
     a.status = status; a.spin_ns = g_spin_limit_ns;
     const long long split = (long long)p.nx * p.ny - p.whole, tiles = p.whole + split * p.splits;
     if (tiles > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
