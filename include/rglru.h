@@ -384,7 +384,7 @@ int32_t rglru_linear_attention_decode_step(const rglru_linear_attention_shape_t 
 /*
  * Gradients of rglru_linear_attention_prefill for upstream gradients do [B,T,H,dv] on o and (optional) ds_T [B,H,dk,dv] fp32 on s_T:
  *     G_t = scale q_t do_t^T + d G_{t+1} (ds_T at the end),  dq_t = scale S_t do_t,  dk_t = G_t v_t,  dv_t = k_t G_t,  ds0 = d G_1
- *   dq, dk, dv    like q, k, v, out; must not overlap an input or one another
+ *   dq, dk, dv    like q, k, v, out; must not overlap an input or one another (side by side in the rows of one tensor, with the same strides, they do not)
  *   ds0           [B,H,dk,dv] fp32, out, or NULL; must not overlap an input
  */
 int32_t rglru_linear_attention_backward(const rglru_linear_attention_shape_t *shape, const rglru_linear_attention_strides_t *strides, const void *q,

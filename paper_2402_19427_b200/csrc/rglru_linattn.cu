@@ -1,5 +1,7 @@
 // Linear attention with a decay for each head: extern "C" entry points, the kernel for any type and width on the CUDA cores, and the
 // decode step.  rglru_linattn.cuh has the mathematics.
+#include <climits>
+
 #include <cuda_bf16.h>
 
 #include "rglru_linattn.cuh"
@@ -354,6 +356,15 @@ bool place(const void *p, const rglru_stride_t &st, const rglru_linear_attention
     bytes = ((size_t)(B - 1) * t.batch + (size_t)(T - 1) * t.token + row) * io_bytes(s->io);
     return by_token || by_batch;
 }
+// Whether two tensors of which each token's row is `row_a` and `row_b` elements long keep clear of one another: apart, or side by side in the same rows
+bool clear_of(const MixTensor &a, size_t a_bytes, long long row_a, const MixTensor &b, size_t b_bytes, long long row_b, const rglru_linear_attention_shape_t *s) {
+    if (!overlap(a.p, a_bytes, b.p, b_bytes)) return true;
+    if ((uintptr_t)a.p > (uintptr_t)b.p) return clear_of(b, b_bytes, row_b, a, a_bytes, row_a, s);
+    if ((s->T > 1 && a.token != b.token) || (s->B > 1 && a.batch != b.batch)) return false;
+    const long long token = s->T > 1 ? a.token : LLONG_MAX, batch = s->B > 1 ? a.batch : LLONG_MAX, inner = token < batch ? token : batch;
+    const long long off = (long long)(((uintptr_t)b.p - (uintptr_t)a.p) / io_bytes(s->io));
+    return off >= row_a && off <= inner - row_b;
+}
 const rglru_linear_attention_strides_t DENSE{};
 size_t state_bytes(const rglru_linear_attention_shape_t *s) { return (size_t)s->B * s->H * s->dk * s->dv * sizeof(float); }
 bool may_use_tensor_cores(const rglru_linear_attention_shape_t *s) {
@@ -473,8 +484,9 @@ int32_t rglru_linear_attention_backward(const rglru_linear_attention_shape_t *s,
     for (int i = 0; i < 4; ++i)
         for (int j = 0; j < 6; ++j)
             if (overlap(outs[i], out_bytes[i], ins[j], in_bytes[j])) return RGLRU_ERR_ALIAS;
-    // dq, dk and dv may lie side by side in one gradient of a projection, tokens interleaved; the same place twice is refused
-    if (dq == dk || dq == dv || dk == dv || overlap(ds0, mat, dq, n[4]) || overlap(ds0, mat, dk, n[5]) || overlap(ds0, mat, dv, n[6])) return RGLRU_ERR_ALIAS;
+    // dq, dk and dv may lie side by side in one gradient of a projection, tokens interleaved
+    const long long rk = (long long)s->H * s->dk, rv = (long long)s->H * s->dv;
+    if (!clear_of(t[4], n[4], rk, t[5], n[5], rk, s) || !clear_of(t[4], n[4], rk, t[6], n[6], rv, s) || !clear_of(t[5], n[5], rk, t[6], n[6], rv, s) || overlap(ds0, mat, dq, n[4]) || overlap(ds0, mat, dk, n[5]) || overlap(ds0, mat, dv, n[6])) return RGLRU_ERR_ALIAS;
     MixArgs a{};
     a.roles = 3; a.B = s->B; a.T = s->T; a.H = s->H; a.log_decay = log_decay; a.status = (uint32_t *)workspace;
     a.role[0] = MixRole{t[3], t[2], t[1], t[4], s->dv, s->dk, s0, nullptr, 1, 0, 1, s->scale, s->scale, 1.0f};

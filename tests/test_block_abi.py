@@ -144,3 +144,25 @@ def test_binding_names_the_wrong_argument(b):
         b.linear_attention_prefill(q, q, q, torch.zeros(2))
     with pytest.raises(TypeError, match="log_decay"):
         b.linear_attention_decode_step(q[:, 0], q[:, 0], q[:, 0], None, q)
+
+
+def test_gradients_side_by_side(b):
+    """dq, dk and dv may be parts of one row (the GPU tests run them so), but no byte of one may lie in another"""
+    lib, S, St = b.load(), b.LinearAttentionShape, b.LinearAttentionStrides
+    for token, batch in ((2 * 128 + 64, 16 * 320), (2 * 320, 320)):   # [B,T,320] and [T,B,320]
+        st = St()
+        for name in ("dq", "dk", "dv"):
+            getattr(st, name)[0], getattr(st, name)[1] = token, batch
+
+        def bwd(dq, dk, dv, n, st=st):
+            shape = S(2, 16, 2, 64, 32, b.BF16, 0.125, 0)
+            return lib.rglru_linear_attention_backward(ctypes.byref(shape), ctypes.byref(st), at(0), at(1), at(2), at(3), at(4), at(5), at(6), at(7, dq), at(7, dk), at(7, dv),
+                                                       at(10), at(11), n, None)
+
+        big = 1 << 30
+        for dq, dk, dv in ((0, 240, 512), (0, 256, 496), (0, 256, 528), (0, 0, 512), (256, 0, 256), (0, 256, 256), (0, 256, 640 * 3 + 512 - 16), (512 + 16, 0, 256)):
+            assert bwd(dq, dk, dv, big) == b.ERR_ALIAS, (dq, dk, dv)
+    other = St()
+    for name, token in (("dq", 320), ("dk", 320), ("dv", 640)):
+        getattr(other, name)[0], getattr(other, name)[1] = token, 32 * token
+    assert bwd(0, 256, 512, big, other) == b.ERR_ALIAS
