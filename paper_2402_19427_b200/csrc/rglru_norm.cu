@@ -163,8 +163,8 @@ template <typename T, int VE, int V> __device__ __forceinline__ void store_vecto
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { return fma2(a, pack2(1.0f, 1.0f), b); }
 __device__ __forceinline__ f32x2 both(float x) { return pack2(x, x); }
 
-// Rows of at most G V VE elements (327680 x 128 bf16: 29 us for 168 MB, 86 % of the copy rate; 16384 x 4096: 47 us for 268 MB).  Thread t of a group holds the vectors t, t + G, ... of its row, the weights of its columns, and its next
-// row's vectors on their way.
+// Rows of at most G V VE elements.  Thread t of a group holds the vectors t, t + G, ... of its row, the weights of its columns, and its next
+// row's vectors on their way.  327680 x 128 bf16: 30 us for 168 MB, 86 % of the copy rate; 16384 x 4096: 47 us for 268 MB.
 template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a) {
     __shared__ float red[2][1][16];
     constexpr int PAIRS = VE * V / 2;
@@ -236,7 +236,8 @@ __device__ __forceinline__ uint4 own16(uint32_t src) {
 }
 constexpr int AHEAD = 3;   // rows that a wide row's threads have on their way in shared memory (one in registers: 16384 x 4096 bf16 83 us instead of 72)
 
-// The gradients, rows as above (16384 x 4096 bf16: 76 us for 403 MB, 79 % of the copy rate; dx alone 71).  The column sums of a group's rows stay in registers and leave once, added over the block's groups.
+// The gradients, rows as above.  The column sums of a group's rows stay in registers and leave once, added over the block's groups.  16384 x 4096
+// bf16: 76 us for 403 MB, 79 % of the copy rate; dx alone 71.
 template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_backward_kernel(NormArgs a) {
     __shared__ float red[2][2][16];
     extern __shared__ float cols[];   // narrow rows: [2][N] sums of the block
