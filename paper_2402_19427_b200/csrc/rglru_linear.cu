@@ -276,6 +276,8 @@ LinearProduct dw_product(const rglru_linear_shape_t *s, const void *dz, const vo
     return {{dz, s->M, s->N, true}, {x, s->M, s->K, true}, s->N, s->K, s->M, s->io, {nullptr, nullptr, dweight, nullptr, RGLRU_ACT_NONE}};
 }
 bool forced_generic(const rglru_linear_shape_t *s) { return s->flags & RGLRU_FLAG_FORCE_GENERIC; }
+// dz in the tensor cores' form
+size_t dz_packed_bytes(const rglru_linear_shape_t *s) { return forced_generic(s) ? 0 : sm100_linear_packed_bytes({nullptr, s->M, s->N, false}, s->io); }
 size_t product_bytes(const rglru_linear_shape_t *s, const LinearProduct &g) { return forced_generic(s) ? 0 : sm100_linear_bytes(g); }
 // Up to eight rows of fp32 (8 x 2560 x 2560: 16 us, on the tensor cores 31), of bf16 while the products are few beside the weights' bytes: one row always (2560 x
 // 2560 5.0 and 8.3 us), more up to 2^25 products (4 x 2560 x 2560 9.9 and 10.2, 6 rows 17 and 10; 8 x 512 x 1024 4.8 and 6.6)
@@ -311,8 +313,10 @@ size_t rglru_linear_workspace_bytes(const rglru_linear_shape_t *s, int32_t op) {
     if (op == RGLRU_OP_PREFILL) return WS_HEADER_BYTES + product_bytes(s, forward_product(s, nullptr, nullptr, {}));
     size_t bytes = WS_HEADER_BYTES + up256((size_t)dz_blocks(s) * s->N * sizeof(float));
     if (s->activation != RGLRU_ACT_NONE) bytes += up256((size_t)s->M * s->N * io_bytes(s->io));
-    const size_t dx = product_bytes(s, dx_product(s, nullptr, nullptr, nullptr)), dw = product_bytes(s, dw_product(s, nullptr, nullptr, nullptr));
-    return bytes + (dx > dw ? dx : dw);   // one after the other
+    LinearProduct gx = dx_product(s, nullptr, nullptr, nullptr), gw = dw_product(s, nullptr, nullptr, nullptr);
+    gx.a.packed = gw.a.packed = &gx;   // in a place of its own, if anywhere
+    const size_t dx = product_bytes(s, gx), dw = product_bytes(s, gw);
+    return bytes + dz_packed_bytes(s) + (dx > dw ? dx : dw);   // one after the other; both read dz
 }
 
 int32_t rglru_linear(const rglru_linear_shape_t *s, const void *x, const void *weight, const float *bias, const void *residual, void *y, void *preact,
@@ -370,8 +374,15 @@ int32_t rglru_linear_backward(const rglru_linear_shape_t *s, const void *dy, con
         add_reduce_job(jobs, part, dz_blocks(s), s->N, dbias, s->N, nullptr, 0, nullptr, 0);
         e = run_reduce_jobs(jobs, st);
     }
-    if (e == cudaSuccess && dx) e = run_product(s, dx_product(s, dz, weight, dx), scratch, workspace, st);
-    if (e == cudaSuccess && dweight) e = run_product(s, dw_product(s, dz, x, dweight), scratch, workspace, st);
+    LinearProduct gx = dx_product(s, dz, weight, dx), gw = dw_product(s, dz, x, dweight);
+    const size_t packed = dz_packed_bytes(s);
+    if (packed) {
+        gx.a.packed = gw.a.packed = scratch;
+        gw.a.ready = dx != nullptr;
+        scratch += packed;
+    }
+    if (e == cudaSuccess && dx) e = run_product(s, gx, scratch, workspace, st);
+    if (e == cudaSuccess && dweight) e = run_product(s, gw, scratch, workspace, st);
     return call_status(e);
 }
 

@@ -23,6 +23,9 @@ struct LinearOperand {
     const void *p;
     long long rows, cols;
     bool turned;
+    // Where the tensor cores' form of the operand lies (sm100_linear_packed_bytes of it) if two products share it, and whether it is there already
+    void *packed = nullptr;
+    bool ready = false;
 };
 struct LinearProduct {
     LinearOperand a, b;
@@ -32,6 +35,8 @@ struct LinearProduct {
 };
 // The scratch that the product takes
 size_t sm100_linear_bytes(const LinearProduct &g);
+// what an operand takes besides, 0 if it is read where it lies
+size_t sm100_linear_packed_bytes(const LinearOperand &o, int io);
 cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status, cudaStream_t st);
 
 // Activations and their slopes, to fp32's last places for fp32 io.  What goes to bf16 takes Phi from the rational approximation 7.1.26 of

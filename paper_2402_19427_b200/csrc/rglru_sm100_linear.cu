@@ -437,7 +437,10 @@ struct Plan {
     size_t a_bytes, b_bytes, part_bytes;
 };
 inline bool f32(const LinearProduct &g) { return g.io == RGLRU_F32; }
-size_t packed_bytes(const LinearOperand &o, bool is_f32) { return up256((size_t)(is_f32 ? PLANES : 1) * o.rows * ((o.cols + 7) / 8 * 8) * 2); }
+size_t packed_bytes(const LinearOperand &o, bool is_f32) {
+    if (!is_f32 && o.cols % 8 == 0) return 0;
+    return up256((size_t)(is_f32 ? PLANES : 1) * o.rows * ((o.cols + 7) / 8 * 8) * 2);
+}
 Plan make_plan(const LinearProduct &g) {
     Plan p{};
     p.swapped = g.M <= 128 && g.N > g.M;
@@ -464,10 +467,10 @@ Plan make_plan(const LinearProduct &g) {
             }
         }
     }
-    p.pack_a = f32(g) || a.cols % 8 != 0;
-    p.pack_b = f32(g) || b.cols % 8 != 0;
-    p.a_bytes = p.pack_a ? packed_bytes(a, f32(g)) : 0;
-    p.b_bytes = p.pack_b ? packed_bytes(b, f32(g)) : 0;
+    p.pack_a = packed_bytes(a, f32(g)) != 0;
+    p.pack_b = packed_bytes(b, f32(g)) != 0;
+    p.a_bytes = a.packed ? 0 : packed_bytes(a, f32(g));
+    p.b_bytes = b.packed ? 0 : packed_bytes(b, f32(g));
     p.part_bytes = (size_t)((long long)p.nx * p.ny - p.whole) * p.splits * 256 * p.NT * sizeof(float);
     return p;
 }
@@ -476,7 +479,8 @@ Plan make_plan(const LinearProduct &g) {
 cudaError_t place(const LinearOperand &o, int io, bool pack, void *at, int box_rows, CUtensorMap *tm, cudaStream_t st) {
     const long long ld = (o.cols + 7) / 8 * 8;
     const int planes = pack && io == RGLRU_F32 ? PLANES : 1;
-    if (pack) {
+    if (pack && o.packed) at = o.packed;
+    if (pack && !o.ready) {
         PackArgs a{o.p, (__nv_bfloat16 *)at, o.rows, o.rows * ld, (int)o.cols, (int)ld};
         const long long blocks = (o.rows * (ld / 8) + 255) / 256;
         if (blocks > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
@@ -516,6 +520,8 @@ struct Device {
 } g_device;
 
 }  // namespace
+
+size_t sm100_linear_packed_bytes(const LinearOperand &o, int io) { return packed_bytes(o, io == RGLRU_F32); }
 
 size_t sm100_linear_bytes(const LinearProduct &g) {
     const Plan p = make_plan(g);
