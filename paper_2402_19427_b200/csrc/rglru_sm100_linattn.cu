@@ -45,8 +45,8 @@ constexpr uint32_t SM_Q = 0, SM_K = TILE, SM_V = SM_K + 2 * TILE, SM_S = SM_V + 
 __host__ __device__ constexpr uint32_t slot_at(int piece) { return piece < 2 ? SM_PLANES + piece * SLOT : SM_S + (piece - 2) * SLOT; }
 static_assert(2 * SLOT <= TILE, "slots in S's place");
 enum { QF, QE, SC, PR, DSF, UR, SR, OE, KF, VF = KF + 2, VK = VF + 2, KVE = VK + 2, PLE = KVE + 2, PLF = PLE + 1, NBAR = PLF + PIECES };   // two of each for the two tiles of k and v
-constexpr uint32_t SM_TMEM = SM_BAR + NBAR * 8, SM_BAD = SM_TMEM + 16,
-                   SM_TOTAL = SM_BAD + 8 * 132, SM_ALLOC = SM_TOTAL + 1024;
+constexpr uint32_t SM_TMEM = SM_BAR + (NBAR + 1) / 2 * 16, SM_BAD = SM_TMEM + 16,
+                   SM_STEPS = (SM_BAD + 8 * 132 + 15) / 16 * 16, SM_TOTAL = SM_STEPS + 64, SM_ALLOC = SM_TOTAL + 1024;
 static_assert(SM_ALLOC <= 232448, "shared memory of a block");
 constexpr uint32_t TM_P = 0, TM_Y = 128, TM_X = 256, TM_U = 384;   // tensor-memory columns
 constexpr int WALKERS = 148;                     // the plan, and with it the workspace, does not depend on the device
@@ -55,12 +55,14 @@ struct WalkArgs {
     alignas(64) CUtensorMap tm[3][3];            // q, k, v of each role: [B][T][H][width]
     MixArgs m;
     int units, chunks;                           // (role, sequence, head), chunks of each
-    int walkers;
-    float *local;                                // [walkers][32][128][4] sums of stretches, or null: no sequence is cut
+    int walkers, rounds, rest;                   // blocks; units that each takes whole, and units left over, which are cut over all blocks
+    int whole_steps;                             // rounds times chunks
+    float *local, *starts;                       // [walkers][32][128][4] sums of stretches, and the states in front of them; null: no sequence is cut
     unsigned long long spin_ns;
 };
-// chunks [first, last) of the walk that block w takes, counted over all units
-__device__ __forceinline__ long long share(const WalkArgs &p, int w) { return (long long)p.units * p.chunks * w / p.walkers; }
+// the first chunk of block w's stretch of the units left over, counted over those
+__device__ __forceinline__ long long share(const WalkArgs &p, int w) { return (long long)p.rest * p.chunks * w / p.walkers; }
+__device__ __forceinline__ long long left_over(const WalkArgs &p) { return (long long)p.rounds * p.walkers * p.chunks; }   // their first chunk, over all units
 
 // One chunk of the walk; next() goes on to the one behind it
 struct Step {
@@ -70,9 +72,11 @@ struct Step {
         n = min(CH, p.m.T - chunk * CH);
         t0 = p.m.role[role].reverse ? p.m.T - (chunk + 1) * CH : chunk * CH;
     }
-    __device__ __forceinline__ Step(const WalkArgs &p, long long g) {
-        const int unit = (int)(g / p.chunks), bh = p.m.B * p.m.H;
-        chunk = (int)(g % p.chunks);
+    __device__ __forceinline__ Step() {}
+    __device__ __forceinline__ Step(const WalkArgs &p, long long g) : Step(p, (int)(g / p.chunks), (int)(g % p.chunks)) {}   // chunk g of all
+    __device__ __forceinline__ Step(const WalkArgs &p, int unit, int in) {
+        const int bh = p.m.B * p.m.H;
+        chunk = in;
         role = unit / bh;
         b = unit % bh / p.m.H;
         h = unit % p.m.H;
@@ -93,6 +97,23 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
+}
+// A step that was left in shared memory: the divisions behind it are done once a block
+__device__ __forceinline__ Step step_at(uint32_t a) {
+    const uint4 x = lds128(a), y = lds128(a + 16);
+    Step st;
+    st.role = (int)x.x; st.b = (int)x.y; st.h = (int)x.z; st.chunk = (int)x.w; st.n = (int)y.x; st.t0 = (int)y.y;
+    st.fresh = true;
+    return st;
+}
+__device__ __forceinline__ void leave_step(int *to, const Step &st) { to[0] = st.role; to[1] = st.b; to[2] = st.h; to[3] = st.chunk; to[4] = st.n; to[5] = st.t0; }
+// What a block walks: whole units or a stretch; whole units and then a stretch (held to code of its own: two tests and a load a step cost 3 %); a
+// stretch for its sums alone
+enum { ONE, BOTH, SUMS };
+// The step behind the first `done`: whole units first, then the stretch
+template <int MODE> __device__ __forceinline__ void advance(Step &st, const WalkArgs &p, int done, uint32_t stretch) {
+    if (MODE == BOTH && done == p.whole_steps) st = step_at(stretch);
+    else st.next(p);
 }
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -132,7 +153,8 @@ __device__ __forceinline__ void load_tile(const WalkArgs &p, int which, const St
 }
 
 // STATE_ONLY: the sums U of a block's last stretch, for the blocks that go on in the same sequence
-template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kernel(const __grid_constant__ WalkArgs p) {
+template <int MODE> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kernel(const __grid_constant__ WalkArgs p) {
+    constexpr bool STATE_ONLY = MODE == SUMS;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw), base = (raw_addr + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (base - raw_addr);
@@ -151,6 +173,21 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid == 32) {   // the block's first step and its number of steps, and its stretch
+        int *at = (int *)(smem + SM_STEPS);
+        if (MODE != SUMS && p.rest == 0) {
+            leave_step(at, Step(p, (int)blockIdx.x * p.rounds, 0));
+            at[6] = p.whole_steps;
+        } else {
+            long long from = share(p, blockIdx.x);
+            const long long to = share(p, blockIdx.x + 1), begin = to / p.chunks * p.chunks;   // begin: of the unit that the stretch ends in
+            if (MODE == SUMS && begin > from) from = begin;   // nothing to do if it ends with a unit
+            const Step stretch(p, left_over(p) + from);
+            leave_step(at, MODE == BOTH ? Step(p, (int)blockIdx.x * p.rounds, 0) : stretch);
+            leave_step(at + 8, stretch);
+            at[6] = (MODE == BOTH ? p.whole_steps : 0) + (int)(to - from);
+        }
+    }
     if (tid < 8 * 33) bad_base[tid] = tid % 33 == 32 ? 0u : 0xFFFFFFFFu;
     if (warp == MMA_WARP) { tmem_alloc(smem_u32(tmem_base_s), 512); tmem_relinquish(); }
     tc_fence_before();
@@ -160,13 +197,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
     bool ok = true;
     dependency_wait();
 
-    const long long last = share(p, blockIdx.x + 1);
-    long long first = share(p, blockIdx.x);
-    if (STATE_ONLY) {
-        const long long begin = last / p.chunks * p.chunks;   // the unit that the share ends in
-        first = begin > first ? begin : first;                // nothing to do if it ends with a unit: first == last
-    }
-    const int steps = (int)(last - first);
+    const int steps = *(volatile int *)(smem + SM_STEPS + 24);
 
     // (each role takes its registers in its own branch: behind a join, all code would get by with the fewest)
     if (warp > MMA_WARP) {
@@ -176,17 +207,17 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         // ---- copies: k and v one chunk ahead of q
         if (elect_one()) {
             auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
-            Step st(p, first), ahead = st;
+            Step st = step_at(base + SM_STEPS), ahead = st;
             auto load_kv = [&](int s) {
                 const MixRole &r = p.m.role[ahead.role];
                 const int k = s & 1;
                 if (!wait(KVE + k, (s >> 1 & 1) ^ 1)) return;
                 load_tile(p, 1, ahead, r.dk, base + SM_K + k * TILE, BAR(KF + k));
                 load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
-                ahead.next(p);
+                advance<MODE>(ahead, p, s + 1, base + SM_STEPS + 32);
             };
             if (steps > 0) load_kv(0);
-            for (int s = 0; s < steps && ok; ++s, st.next(p)) {
+            for (int s = 0; s < steps && ok; ++s, advance<MODE>(st, p, s, base + SM_STEPS + 32)) {
                 if (!STATE_ONLY && wait(QE, (s & 1) ^ 1)) load_tile(p, 0, st, p.m.role[st.role].dk, base + SM_Q, BAR(QF));
                 if (ok && s + 1 < steps) load_kv(s + 1);
             }
@@ -215,7 +246,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                 }
                 tc_commit(BAR(SC));
             };
-            Step st(p, first);
+            Step st = step_at(base + SM_STEPS);
             if (!STATE_ONLY && steps > 0) scores(0, p.m.role[st.role]);
 #pragma unroll 1
             for (int s = 0; s < steps && ok; ++s) {
@@ -269,7 +300,7 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
                 if (!ok) break;
                 tc_commit(BAR(DSF));   // all of the step's products
                 tc_commit(BAR(KVE + (s & 1)));
-                st.next(p);
+                advance<MODE>(st, p, s + 1, base + SM_STEPS + 32);
                 if (!STATE_ONLY && s + 1 < steps) scores(s + 1, p.m.role[st.role]);
             }
             if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
@@ -305,10 +336,10 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         const int row = warp * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
         float ld = 0.0f, d1 = 0.0f;
-        Step st(p, first), ahead = st;
+        Step st = step_at(base + SM_STEPS), ahead = st;
         if (steps > 0) look_through(0, ahead);
-        for (int s = 0; s < steps && ok; ++s, st.next(p)) {
-            ahead.next(p);
+        for (int s = 0; s < steps && ok; ++s, advance<MODE>(st, p, s, base + SM_STEPS + 32)) {
+            advance<MODE>(ahead, p, s + 1, base + SM_STEPS + 32);
             if (STATE_ONLY) {
                 if (s + 1 < steps) look_through(s + 1, ahead);
                 continue;
@@ -388,8 +419,8 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         const int quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         float far = 0.0f;
-        Step st(p, first);
-        for (int s = 0; !STATE_ONLY && s < steps && ok; ++s, st.next(p)) {
+        Step st = step_at(base + SM_STEPS);
+        for (int s = 0; !STATE_ONLY && s < steps && ok; ++s, advance<MODE>(st, p, s, base + SM_STEPS + 32)) {
             const MixRole &r = p.m.role[st.role];
             const uint32_t ph = s & 1;
             const int i = r.reverse ? CH - 1 - row : row;
@@ -445,33 +476,26 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
         f32x2 S2[32];
         auto at = [&](int j) -> float & { return j & 1 ? S2[j / 2].y : S2[j / 2].x; };
-        auto init_state = [&](const Step &st, long long g) {
+        auto init_state = [&](const Step &st) {
             const MixRole &r = p.m.role[st.role];
             const long long mat = (long long)(st.b * p.m.H + st.h) * r.dk * r.dv;
             const float *src = STATE_ONLY ? nullptr : r.s_in;
+            if (!STATE_ONLY && st.chunk != 0) {   // inside a sequence: the state was left there
+                const float4 *l = (const float4 *)p.starts + ((size_t)blockIdx.x * 32 + e0 / 4) * 128 + d;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float4 v = l[j * 128];
+                    S2[2 * j] = pack2(v.x, v.y);
+                    S2[2 * j + 1] = pack2(v.z, v.w);
+                }
+                return;
+            }
 #pragma unroll
             for (int j = 0; j < 32; ++j) S2[j] = pack2(0.0f, 0.0f);
             if (src && d < r.dk) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
                     if (e0 + j < r.dv) at(j) = src[mat + (r.turned ? (long long)(e0 + j) * r.dk + d : (long long)d * r.dv + e0 + j)];
-            }
-            if (!STATE_ONLY && st.chunk != 0) {   // the stretches in front of this one, block by block
-                const long long begin = g - st.chunk;
-                int w = (int)(begin * p.walkers / ((long long)p.units * p.chunks));
-                while (share(p, w + 1) <= begin) ++w;
-                for (; w < (int)blockIdx.x; ++w) {
-                    const long long from = share(p, w) > begin ? share(p, w) : begin, to = share(p, w + 1);
-                    const float f = decay_power(p.m.log_decay[st.h], (float)((to - from) * CH));
-                    const float4 *l = (const float4 *)p.local + ((size_t)w * 32 + e0 / 4) * 128 + d;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        if (j % 4 == 0) asm volatile("" ::: "memory");   // four loads at a time: registers
-                        const float4 v = l[j * 128];
-                        S2[2 * j] = fma2(pack2(f, f), S2[2 * j], pack2(v.x, v.y));
-                        S2[2 * j + 1] = fma2(pack2(f, f), S2[2 * j + 1], pack2(v.z, v.w));
-                    }
-                }
             }
         };
         // S to shared memory for the far product: rows of 64 columns, 16-byte pieces swizzled as a tiled copy would have them; sixteen
@@ -489,15 +513,15 @@ template <bool STATE_ONLY> __global__ void __launch_bounds__(THREADS, 1) mix_wal
             if (lane == 0) mbar_arrive(BAR(SR));
         };
         float ld = 0.0f;
-        Step st(p, first);
+        Step st = step_at(base + SM_STEPS);
 #pragma unroll 1
-        for (int s = 0; s < steps && ok; ++s, st.next(p)) {
+        for (int s = 0; s < steps && ok; ++s, advance<MODE>(st, p, s, base + SM_STEPS + 32)) {
             const MixRole &r = p.m.role[st.role];
             const uint32_t ph = s & 1;
             uint32_t *bad = bad_base + (s & 7) * 33;
             if (st.fresh) {
                 ld = p.m.log_decay[st.h];
-                init_state(st, first + s);
+                init_state(st);
                 if (!STATE_ONLY) {
 #pragma unroll
                     for (int c = 0; c < 64; c += 16) put16(c);
@@ -564,9 +588,9 @@ if (STATE_ONLY && steps > 0 && ok) {
         const int k_tid = tid - K_FIRST * 32;
         float weight = 0.0f;
         int n_tokens = 0;
-        Step st(p, first);
+        Step st = step_at(base + SM_STEPS);
 #pragma unroll 1
-        for (int s = 0; s < steps && ok; ++s, st.next(p)) {
+        for (int s = 0; s < steps && ok; ++s, advance<MODE>(st, p, s, base + SM_STEPS + 32)) {
             const MixRole &r = p.m.role[st.role];
             const uint32_t ph = s & 1;
             if (st.fresh || st.n != n_tokens) {   // lane (8 i + m) of a warp: the weight decay^(n - j - first) of the warp's row i + 16 m
@@ -634,13 +658,55 @@ if (STATE_ONLY && steps > 0 && ok) {
     if (warp == MMA_WARP) tmem_dealloc(tmem, 512);
 }
 
-// Blocks: one a (role, sequence, head) while that is as fast, else 148 with equal shares.  In chunks: a block's own, and for cut
-// sequences half of its last stretch again (state only) and some four for the second launch and the states read.
-int plan_walkers(int roles, int B, int T, int H) {
-    const long long units = (long long)roles * B * H, chunks = (T + CH - 1) / CH, all = units * chunks;
-    const long long whole = (units + WALKERS - 1) / WALKERS * chunks;
-    const long long share = (all + WALKERS - 1) / WALKERS, cut = share + (share < chunks ? share : chunks / 2) / 2 + 4;
-    return whole <= cut || all < WALKERS ? (int)units : WALKERS;
+// From the sums of stretches to the states in front of them, sequence by sequence: a thread has four columns of a row, the sums of eight stretches on
+// their way.
+__global__ void __launch_bounds__(256) mix_fold_kernel(const __grid_constant__ WalkArgs p) {
+    dependency_wait();
+    const int unit = blockIdx.x / 16, item = blockIdx.x % 16 * 256 + threadIdx.x, d = item % 128, e0 = item / 128 * 4;
+    const long long begin = (long long)unit * p.chunks, end = begin + p.chunks;
+    const Step st(p, left_over(p) + begin);
+    const MixRole &r = p.m.role[st.role];
+    const float ld = p.m.log_decay[st.h];
+    float s[4] = {};
+    if (r.s_in && d < r.dk) {
+        const float *src = r.s_in + (long long)(st.b * p.m.H + st.h) * r.dk * r.dv;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (e0 + j < r.dv) s[j] = src[r.turned ? (long long)(e0 + j) * r.dk + d : (long long)d * r.dv + e0 + j];
+    }
+    int w = (int)(begin * p.walkers / ((long long)p.rest * p.chunks));
+    while (share(p, w + 1) <= begin) ++w;
+    const size_t at = (size_t)(item / 128) * 128 + d;
+    for (; w < p.walkers && share(p, w) < end; w += 8) {
+        float4 sums[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (w + k < p.walkers && share(p, w + k + 1) < end) sums[k] = ((const float4 *)p.local)[(size_t)(w + k) * 4096 + at];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (w + k >= p.walkers) break;
+            const long long from = share(p, w + k), to = share(p, w + k + 1);
+            if (from >= end || from == to) continue;   // (with fewer chunks than blocks some have none, and leave no sums)
+            if (from > begin) ((float4 *)p.starts)[(size_t)(w + k) * 4096 + at] = make_float4(s[0], s[1], s[2], s[3]);
+            if (to < end) {
+                const float f = decay_power(ld, (float)((to - (from > begin ? from : begin)) * CH));
+                s[0] = fmaf(f, s[0], sums[k].x); s[1] = fmaf(f, s[1], sums[k].y); s[2] = fmaf(f, s[2], sums[k].z); s[3] = fmaf(f, s[3], sums[k].w);
+            }
+        }
+    }
+    dependency_trigger();
+}
+
+// Blocks: one a (role, sequence, head) while that is as fast, else 148: each takes as many whole ones as there are for all, and an equal stretch of the
+// rest.  In chunks: a block's own, and for stretches half of theirs again (sums only) and some six for two more launches and the states read.
+// (Stretches of everything, in one order, cost sums of half a sequence a block: 8 x 2048 tokens of 20 heads took 139 us.)
+struct WalkPlan { int walkers, rounds, rest; };
+WalkPlan walk_plan(int roles, int B, int T, int H) {
+    const long long units = (long long)roles * B * H, chunks = (T + CH - 1) / CH;
+    const long long rounds = units / WALKERS, rest = units % WALKERS, share = (rest * chunks + WALKERS - 1) / WALKERS;
+    const long long whole = (rounds + (rest != 0)) * chunks, cut = rounds * chunks + share + share / 2 + 6;
+    if (whole <= cut || units * chunks < WALKERS) return {(int)units, 1, 0};
+    return {WALKERS, (int)rounds, (int)rest};
 }
 
 }  // namespace
@@ -657,8 +723,8 @@ bool sm100_mix_supported(const MixArgs &a, int io) {
 }
 
 size_t sm100_mix_bytes(int roles, int B, int T, int H) {
-    const int w = plan_walkers(roles, B, T, H);
-    return w == roles * B * H ? 0 : (size_t)w * 128 * 128 * sizeof(float);
+    const WalkPlan w = walk_plan(roles, B, T, H);
+    return w.rest == 0 ? 0 : (size_t)w.walkers * 128 * 128 * 2 * sizeof(float);
 }
 
 cudaError_t sm100_mix(const MixArgs &a, void *scratch, cudaStream_t st) {
@@ -666,9 +732,12 @@ cudaError_t sm100_mix(const MixArgs &a, void *scratch, cudaStream_t st) {
     p.m = a;
     p.units = a.roles * a.B * a.H;
     p.chunks = (a.T + CH - 1) / CH;
-    p.walkers = plan_walkers(a.roles, a.B, a.T, a.H);
-    const bool cut = p.walkers != p.units;
+    const WalkPlan plan = walk_plan(a.roles, a.B, a.T, a.H);
+    p.walkers = plan.walkers; p.rounds = plan.rounds; p.rest = plan.rest;
+    const bool cut = p.rest != 0;
+    p.whole_steps = p.rounds * p.chunks;
     p.local = cut ? (float *)scratch : nullptr;
+    p.starts = cut ? p.local + (size_t)p.walkers * 128 * 128 : nullptr;
     p.spin_ns = g_spin_limit_ns;
     for (int i = 0; i < a.roles; ++i) {
         const MixRole &r = a.role[i];
@@ -682,11 +751,13 @@ cudaError_t sm100_mix(const MixArgs &a, void *scratch, cudaStream_t st) {
             if (!encode_map16_4d(&p.tm[i][j], t[j]->p, dims, strides, box, true)) return cudaErrorNotSupported;
         }
     }
-    static PerDeviceOptIn opt_main, opt_state;
-    cudaError_t e = opt_main.ensure(mix_walk_kernel<false>, (int)SM_ALLOC);
-    if (e == cudaSuccess && cut) e = opt_state.ensure(mix_walk_kernel<true>, (int)SM_ALLOC);
-    if (e == cudaSuccess && cut) e = launch_dependent(mix_walk_kernel<true>, dim3(p.walkers), dim3(THREADS), SM_ALLOC, st, p);
-    if (e == cudaSuccess) e = launch_dependent(mix_walk_kernel<false>, dim3(p.walkers), dim3(THREADS), SM_ALLOC, st, p);
+    static PerDeviceOptIn opt_one, opt_both, opt_sums;
+    const bool both = cut && p.rounds != 0;
+    cudaError_t e = both ? opt_both.ensure(mix_walk_kernel<BOTH>, (int)SM_ALLOC) : opt_one.ensure(mix_walk_kernel<ONE>, (int)SM_ALLOC);
+    if (e == cudaSuccess && cut) e = opt_sums.ensure(mix_walk_kernel<SUMS>, (int)SM_ALLOC);
+    if (e == cudaSuccess && cut) e = launch_dependent(mix_walk_kernel<SUMS>, dim3(p.walkers), dim3(THREADS), SM_ALLOC, st, p);
+    if (e == cudaSuccess && cut) e = launch_dependent(mix_fold_kernel, dim3(16 * p.rest), dim3(256), 0, st, p);
+    if (e == cudaSuccess) e = launch_dependent(both ? mix_walk_kernel<BOTH> : mix_walk_kernel<ONE>, dim3(p.walkers), dim3(THREADS), SM_ALLOC, st, p);
     return e;
 }
 

@@ -226,3 +226,17 @@ def test_cut_sequences_whose_state_is_updated_in_place(io, B, T, H, dk, dv):
     off = 2 * bo.state_bound(sm, T)
     bo.assert_within("s_T", s_T, sr, off)
     bo.assert_within("o", o[:, cut:], orr, 2 * bo.attention_bound(om, orr, DT[io], T) + bo.U32 * (512 + T / 8) * om)
+
+
+@pytest.mark.parametrize("B,T,H,dk,dv", [(8, 2000, 20, 64, 32), (3, 1400, 99, 24, 64)])
+def test_more_heads_than_fit_at_once(B, T, H, dk, dv):
+    """Whole sequences for every block and a stretch of those left over, forward and backward"""
+    from paper_2402_19427_b200 import binding
+    t = make(B, T, H, dk, dv, "bf16")
+    o, s_T = binding.linear_attention_prefill(t["q"], t["k"], t["v"], t["ld"], s0=t["s0"])
+    check_forward(t, o, s_T, dk ** -0.5)
+    got = binding.linear_attention_backward(t["q"], t["k"], t["v"], t["ld"], t["do"], s0=t["s0"], ds_T=t["ds_T"], state_grads=True)
+    check_backward(t, got, dk ** -0.5)
+    s = t["s0"].clone()
+    o2, _ = binding.linear_attention_prefill(t["q"], t["k"], t["v"], t["ld"], s0=s, s_T=s)
+    assert torch.equal(o, o2) and torch.equal(s, s_T)
