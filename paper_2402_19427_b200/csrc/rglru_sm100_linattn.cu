@@ -17,8 +17,9 @@
 // Outputs go from registers to memory, 32 bytes a thread: staged in shared memory for a tiled copy they held v's place for
 // another 4000 cycles a chunk.
 //
-// Blocks share the chunks of all (role, sequence, head) evenly, in order; a block that begins inside a sequence takes the state before it
-// from the sums that a first launch (planes and state product only) leaves for the stretches in front of it.
+// Each block walks as many whole (role, sequence, head) as there are for all, and an equal stretch of the chunks of those left over.  The state in front
+// of a stretch comes from two small launches: one leaves the sums of every stretch's last sequence (planes and state product only, 2.3 us a
+// chunk), one folds them in order.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
