@@ -195,3 +195,21 @@ def test_two_graphs_in_one_workspace(io):
             graph.replay()
             fe, ge = step()
             assert all(torch.equal(a, b) for a, b in zip(flat(f) + flat(g), flat(fe) + flat(ge)))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_two_streams_at_once(io):
+    """Two users' blocks on streams of their own, each with its workspace, while the default stream idles"""
+    p = params(io)
+    users = [(inputs(T, io, seed), workspace(), torch.cuda.Stream()) for T, seed in ((260, 4), (150, 5))]
+    step = lambda x, s0, dout, ws: (lambda f: flat(f) + flat(backward(p, x, s0, f, dout, ws)))(forward(p, x, s0, ws))  # noqa: E731
+    alone = [step(*data, ws) for data, ws, _ in users]
+    torch.cuda.synchronize()
+    results = [[], []]
+    for _ in range(5):
+        for i, (data, ws, stream) in enumerate(users):
+            with torch.cuda.stream(stream):
+                results[i].append(step(*data, ws))
+    torch.cuda.synchronize()
+    for runs, want in zip(results, alone):
+        assert all(torch.equal(a, b) for run in runs for a, b in zip(run, want))
