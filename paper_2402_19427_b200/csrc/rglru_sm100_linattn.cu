@@ -438,6 +438,7 @@ template <int MODE> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kerne
 #pragma unroll 1
             for (int c = 0; c < r.dv; c += 16) {
                 f32x2 y[8], x[8];
+                __syncwarp();   // lanes part at a ragged chunk's stores below, and tensor memory is read by whole warps
                 tmem_ld16(lanes + TM_Y + c, y);
                 tmem_ld16(lanes + TM_X + c, x);
                 tmem_ld_wait();
