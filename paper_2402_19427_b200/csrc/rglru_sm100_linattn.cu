@@ -200,111 +200,110 @@ template <int MODE> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kerne
 
     const int steps = *(volatile int *)(smem + SM_STEPS + 24);
 
-    // (each role takes its registers in its own branch: behind a join, all code would get by with the fewest)
-    if (warp > MMA_WARP) {
-        reg_dec<40>();
-    } else if (warp == COPY_WARP) {
-        reg_dec<40>();
-        // ---- copies: k and v one chunk ahead of q
-        if (elect_one()) {
-            auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
-            Step st = step_at(base + SM_STEPS), ahead = st;
-            auto load_kv = [&](int s) {
-                const MixRole &r = p.m.role[ahead.role];
-                const int k = s & 1;
-                if (!wait(KVE + k, (s >> 1 & 1) ^ 1)) return;
-                load_tile(p, 1, ahead, r.dk, base + SM_K + k * TILE, BAR(KF + k));
-                load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
-                advance<MODE>(ahead, p, s + 1, base + SM_STEPS + 32);
-            };
-            if (steps > 0) load_kv(0);
-            for (int s = 0; s < steps && ok; ++s, advance<MODE>(st, p, s, base + SM_STEPS + 32)) {
-                if (!STATE_ONLY && wait(QE, (s & 1) ^ 1)) load_tile(p, 0, st, p.m.role[st.role].dk, base + SM_Q, BAR(QF));
-                if (ok && s + 1 < steps) load_kv(s + 1);
-            }
-            if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
-        }
-    } else if (warp == MMA_WARP) {
-        reg_dec<40>();
-        // ---- products
-        // Waits never suspend the thread: what it waits for is tens of cycles away, waking up takes hundreds.
-        if (elect_one()) {
-            auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); };
-            // Descriptors are counted on from step to step (16 bytes are one unit of their address field): held for all steps at once they
-            // would not fit this warpgroup's registers.
-            auto kmajor = [&](uint32_t at) { return make_desc_sw128(base + at); };
-            auto turned = [&](uint32_t at, uint32_t block) { return make_desc_sw128_mn(base + at, block); };
-            auto scores = [&](int s, const MixRole &r) {
-                wait(QF, s & 1); wait(KF + (s & 1), s >> 1 & 1);
-                if (!ok) return;
-                tc_fence_after();
-                const uint32_t id = make_idesc(128, 128);
-#pragma unroll 1
-                for (int b = 0; b * 64 < r.dk; ++b) {
-                    const uint64_t q = kmajor(SM_Q + b * BLOCK), k = kmajor(SM_K + (s & 1) * TILE + b * BLOCK);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_P, q + 2 * i, k + 2 * i, id, b | i);
+    // (each warpgroup takes its registers in its own branch: behind a join, all code would get by with the fewest)
+    if (warp >= COPY_WARP) {
+        reg_dec<40>();   // once for all four warps: a warpgroup executes the same setmaxnreg together
+        if (warp == COPY_WARP) {
+            // ---- copies: k and v one chunk ahead of q
+            if (elect_one()) {
+                auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
+                Step st = step_at(base + SM_STEPS), ahead = st;
+                auto load_kv = [&](int s) {
+                    const MixRole &r = p.m.role[ahead.role];
+                    const int k = s & 1;
+                    if (!wait(KVE + k, (s >> 1 & 1) ^ 1)) return;
+                    load_tile(p, 1, ahead, r.dk, base + SM_K + k * TILE, BAR(KF + k));
+                    load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
+                    advance<MODE>(ahead, p, s + 1, base + SM_STEPS + 32);
+                };
+                if (steps > 0) load_kv(0);
+                for (int s = 0; s < steps && ok; ++s, advance<MODE>(st, p, s, base + SM_STEPS + 32)) {
+                    if (!STATE_ONLY && wait(QE, (s & 1) ^ 1)) load_tile(p, 0, st, p.m.role[st.role].dk, base + SM_Q, BAR(QF));
+                    if (ok && s + 1 < steps) load_kv(s + 1);
                 }
-                tc_commit(BAR(SC));
-            };
-            Step st = step_at(base + SM_STEPS);
-            if (!STATE_ONLY && steps > 0) scores(0, p.m.role[st.role]);
-#pragma unroll 1
-            for (int s = 0; s < steps && ok; ++s) {
-                const MixRole &r = p.m.role[st.role];
-                const uint32_t ph = s & 1, nv = r.dv > 64 ? 128 : 64, id_b = make_idesc(128, nv) | (1u << 16), id_ab = id_b | (1u << 15);
-                const uint32_t v_at = SM_V + (s & 1) * TILE;
-                uint64_t v = turned(v_at, BLOCK);
-                auto piece = [&](int pc) {
-                    wait(PLF + pc, ph);
+                if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
+            }
+        } else if (warp == MMA_WARP) {
+            // ---- products
+            // Waits never suspend the thread: what it waits for is tens of cycles away, waking up takes hundreds.
+            if (elect_one()) {
+                auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); };
+                // Descriptors are counted on from step to step (16 bytes are one unit of their address field): held for all steps at once they
+                // would not fit this warpgroup's registers.
+                auto kmajor = [&](uint32_t at) { return make_desc_sw128(base + at); };
+                auto turned = [&](uint32_t at, uint32_t block) { return make_desc_sw128_mn(base + at, block); };
+                auto scores = [&](int s, const MixRole &r) {
+                    wait(QF, s & 1); wait(KF + (s & 1), s >> 1 & 1);
                     if (!ok) return;
                     tc_fence_after();
-                    const uint64_t first_plane = turned(SM_K + (s & 1) * TILE + pc * 4096, BLOCK), others = turned(slot_at(pc), PLANE / 2);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, others + PLANE / 16 + k * 128, v + k * 128, id_ab, pc | k);   // the smallest first
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, others + k * 128, v + k * 128, id_ab, 1);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, first_plane + k * 128, v + k * 128, id_ab, 1);
-                    v += 256;
+                    const uint32_t id = make_idesc(128, 128);
+    #pragma unroll 1
+                    for (int b = 0; b * 64 < r.dk; ++b) {
+                        const uint64_t q = kmajor(SM_Q + b * BLOCK), k = kmajor(SM_K + (s & 1) * TILE + b * BLOCK);
+    #pragma unroll
+                        for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_P, q + 2 * i, k + 2 * i, id, b | i);
+                    }
+                    tc_commit(BAR(SC));
                 };
-                wait(VK + (s & 1), s >> 1 & 1);
-                wait(UR, ph ^ 1);
-#pragma unroll 1
-                for (int pc = 0; pc < PIECES; ++pc) {
-                    if (!STATE_ONLY && pc == 1) {
-                        wait(SR, ph);
-                        wait(OE, ph ^ 1);   // the last outputs have been read
-                        if (!ok) break;
+                Step st = step_at(base + SM_STEPS);
+                if (!STATE_ONLY && steps > 0) scores(0, p.m.role[st.role]);
+    #pragma unroll 1
+                for (int s = 0; s < steps && ok; ++s) {
+                    const MixRole &r = p.m.role[st.role];
+                    const uint32_t ph = s & 1, nv = r.dv > 64 ? 128 : 64, id_b = make_idesc(128, nv) | (1u << 16), id_ab = id_b | (1u << 15);
+                    const uint32_t v_at = SM_V + (s & 1) * TILE;
+                    uint64_t v = turned(v_at, BLOCK);
+                    auto piece = [&](int pc) {
+                        wait(PLF + pc, ph);
+                        if (!ok) return;
                         tc_fence_after();
-                        uint64_t rows = turned(SM_S, BLOCK);   // S as it lies: rows of 64 columns of v
-#pragma unroll 1
-                        for (int b = 0; b * 64 < r.dk; ++b, rows += 4 * 128) {
-                            const uint64_t q = kmajor(SM_Q + b * BLOCK);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_X, q + 2 * i, rows + 128 * i, id_b, b | i);
+                        const uint64_t first_plane = turned(SM_K + (s & 1) * TILE + pc * 4096, BLOCK), others = turned(slot_at(pc), PLANE / 2);
+    #pragma unroll
+                        for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, others + PLANE / 16 + k * 128, v + k * 128, id_ab, pc | k);   // the smallest first
+    #pragma unroll
+                        for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, others + k * 128, v + k * 128, id_ab, 1);
+    #pragma unroll
+                        for (int k = 0; k < 2; ++k) mma_ss(tmem + TM_U, first_plane + k * 128, v + k * 128, id_ab, 1);
+                        v += 256;
+                    };
+                    wait(VK + (s & 1), s >> 1 & 1);
+                    wait(UR, ph ^ 1);
+    #pragma unroll 1
+                    for (int pc = 0; pc < PIECES; ++pc) {
+                        if (!STATE_ONLY && pc == 1) {
+                            wait(SR, ph);
+                            wait(OE, ph ^ 1);   // the last outputs have been read
+                            if (!ok) break;
+                            tc_fence_after();
+                            uint64_t rows = turned(SM_S, BLOCK);   // S as it lies: rows of 64 columns of v
+    #pragma unroll 1
+                            for (int b = 0; b * 64 < r.dk; ++b, rows += 4 * 128) {
+                                const uint64_t q = kmajor(SM_Q + b * BLOCK);
+    #pragma unroll
+                                for (int i = 0; i < 4; ++i) mma_ss(tmem + TM_X, q + 2 * i, rows + 128 * i, id_b, b | i);
+                            }
+                            tc_commit(BAR(QE));
                         }
-                        tc_commit(BAR(QE));
-                    }
-                    if (pc == 2) tc_commit(BAR(PLE));   // the first two slots have been read
-                    if (!STATE_ONLY && pc == 2) {
-                        wait(PR, ph);
+                        if (pc == 2) tc_commit(BAR(PLE));   // the first two slots have been read
+                        if (!STATE_ONLY && pc == 2) {
+                            wait(PR, ph);
+                            if (!ok) break;
+                            tc_fence_after();
+                            uint64_t rows = turned(v_at, BLOCK);
+    #pragma unroll 4
+                            for (int k = 0; k < 8; ++k, rows += 128) mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, rows, id_b, k);
+                        }
+                        piece(pc);
                         if (!ok) break;
-                        tc_fence_after();
-                        uint64_t rows = turned(v_at, BLOCK);
-#pragma unroll 4
-                        for (int k = 0; k < 8; ++k, rows += 128) mma_ts(tmem + TM_Y, tmem + TM_P + k * 8, rows, id_b, k);
                     }
-                    piece(pc);
                     if (!ok) break;
+                    tc_commit(BAR(DSF));   // all of the step's products
+                    tc_commit(BAR(KVE + (s & 1)));
+                    advance<MODE>(st, p, s + 1, base + SM_STEPS + 32);
+                    if (!STATE_ONLY && s + 1 < steps) scores(s + 1, p.m.role[st.role]);
                 }
-                if (!ok) break;
-                tc_commit(BAR(DSF));   // all of the step's products
-                tc_commit(BAR(KVE + (s & 1)));
-                advance<MODE>(st, p, s + 1, base + SM_STEPS + 32);
-                if (!STATE_ONLY && s + 1 < steps) scores(s + 1, p.m.role[st.role]);
+                if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
             }
-            if (!ok) { *abort_flag = 1; atomicExch(p.m.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
         }
     } else if (warp < P_WARPS) {
         reg_inc<80>();

@@ -19,7 +19,7 @@ def source(name):
 
 
 def blocks(text):
-    """(start, end, header) of every brace block; the header is what stands between the last ; { } and the opening brace"""
+    """(start, end, header, before) of every brace block; the header is what stands between the last ; { } (at `before`) and the opening brace"""
     stack, out = [], []
     for i, c in enumerate(text):
         if c == "{":
@@ -27,10 +27,10 @@ def blocks(text):
             while at >= 0 and (depth or text[at] not in ";{}"):   # (a ; inside the parentheses of a for does not end it)
                 depth += {")": 1, "(": -1}.get(text[at], 0)
                 at -= 1
-            stack.append((i, " ".join(text[at + 1:i].split())))
+            stack.append((i, " ".join(text[at + 1:i].split()), at))
         elif c == "}":
-            start, header = stack.pop()
-            out.append((start, i, header))
+            start, header, before = stack.pop()
+            out.append((start, i, header, before))
     return out
 
 
@@ -45,7 +45,7 @@ def reached_apart(text):
         around = [b for b in all_blocks if b[0] < m.start() < b[1] and is_loop(b[2])]
         if not around:
             continue
-        start, end, _ = max(around)
+        start, end = max(around)[:2]
         before = text[m.end():end] + text[start:m.start()]   # what ran since this access, once around the loop
         apart = [p.end() for p in PARTS.finditer(before)]
         together = [p.start() for p in TOGETHER.finditer(before)]
@@ -63,3 +63,48 @@ def test_the_reader_sees_what_it_should():
 @pytest.mark.parametrize("name", ["rglru_sm100_linattn.cu"])
 def test_tensor_memory_is_read_by_whole_warps(name):
     assert reached_apart(source(name)) == []
+
+
+def conditions(text, at):
+    """The conditions on `warp` under which the code at `at` runs: of its own branch, and the negated ones of the branches before it"""
+    out, all_blocks = [], blocks(text)
+    for start, end, header, before in all_blocks:
+        if not start < at < end:
+            continue
+        chain = []   # this branch's and those of the branches before it
+        while (m := re.fullmatch(r"(else )?if \((.*)\)|(else)", header)):
+            chain.append(m.group(2) or "True")
+            if not (m.group(1) or m.group(3)):
+                break
+            start, _, header, before = next(b for b in all_blocks if b[1] == before)
+        if "warp" in " ".join(chain):
+            out.append(chain)
+    return out
+
+
+def warps_that_run(text, at, names, warps):
+    ran = []
+    for w in range(warps):
+        value = dict(names, warp=w, true=True)
+        if all(eval(c[0], {}, value) and not any(eval(e, {}, value) for e in c[1:]) for c in conditions(text, at)):
+            ran.append(w)
+    return ran
+
+
+def test_register_budgets_are_set_by_whole_warpgroups():
+    """setmaxnreg: all warps of a warpgroup execute the same one"""
+    text = source("rglru_sm100_linattn.cu")
+    names = {}
+    for m in re.finditer(r"constexpr int ([^;]*);", text):
+        for part in m.group(1).split(","):
+            name, value = part.split("=")
+            try:
+                names[name.strip()] = eval(value, {}, names)
+            except (NameError, SyntaxError):
+                pass
+    warps, seen = names["THREADS"] // 32, []
+    for m in re.finditer(r"\breg_(?:dec|inc)<", text):
+        ran = warps_that_run(text, m.start(), names, warps)
+        assert ran and len(ran) % 4 == 0 and all(ran[i] == ran[0] + i for i in range(len(ran))) and ran[0] % 4 == 0, (text[:m.start()].count("\n") + 1, ran)
+        seen += ran
+    assert sorted(seen) == list(range(warps))
