@@ -321,6 +321,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
 #pragma unroll 1
                 for (int c = half * 32; c < p.NT; c += 64) {
                     f32x2 x[16];
+                    __syncwarp();   // lanes part at rows that do not exist below, and tensor memory is read by whole warps
                     tmem_ld32(lanes + acc * 256 + c, x);
                     tmem_ld_wait();
                     float v[32];
