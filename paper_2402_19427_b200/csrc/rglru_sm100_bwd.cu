@@ -219,6 +219,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) tc_gemm_kernel(const __grid_c
                     const int c0 = j * 64 + half * 32;
                     if (c0 < p.NT) {
                         f32x2 v[16];
+                        __syncwarp();   // lanes part at rows that do not exist below, and tensor memory is read by whole warps
                         tmem_ld32(tm_lane + c0, v);
                         tmem_ld_wait();
                         if (valid && c0 < cv) {
@@ -239,6 +240,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) tc_gemm_kernel(const __grid_c
 #pragma unroll 1
                 for (int c0 = half * 32; c0 < p.NT; c0 += 64) {
                     f32x2 v[16];
+                    __syncwarp();
                     tmem_ld32(tm_lane + c0, v);
                     tmem_ld_wait();
                     if (!valid) continue;

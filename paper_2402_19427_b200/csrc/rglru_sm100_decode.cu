@@ -312,6 +312,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) sm100_d
             if (j0 >= nq) break;
             const int n0 = kq * nq + j0;
             float za[4], zx[4];
+            __syncwarp();   // lanes part at the stores below, and tensor memory is read by whole warps
             tmem_ld4(tm_lane + n0, za);
             tmem_ld4(tm_lane + 128 + n0, zx);
             tmem_ld_wait();

@@ -214,6 +214,7 @@ __device__ __noinline__ float2 exact_walk(const SplitFwdArgs &p, uint32_t tm, in
         segP[j] = k.P; segH[j] = k.h;
         const size_t e = ((size_t)b * T + tb) * D + head * dh + c;
         walk_segment<SAVE, false>(k, za, zx, xs, tb, T, D, cv, SAVE ? f.save_r + e : nullptr, SAVE ? f.save_i + e : nullptr);
+        __syncwarp();   // lanes part at what a walk saves, and tensor memory is for whole warps
         if (!SAVE) { tmem_st8p(tm + j * SEG, za); tmem_st8p(tm + 2 * TOK + j * SEG, zx); }
     }
     if (SAVE) {
@@ -289,6 +290,7 @@ __device__ __forceinline__ void forward_rest(const SplitFwdArgs &p, uint32_t tme
 #pragma unroll 1
     for (int j = 0; j < HALF / SEG; ++j) {
         f32x2 Pv[4], hv[4];
+        __syncwarp();   // lanes part at the stores below
         tmem_ld8p(tm + j * SEG, Pv); tmem_ld8p(tm + 2 * TOK + j * SEG, hv);
         tmem_ld_wait();
         const int tb = t0 + j * SEG;
@@ -342,6 +344,7 @@ __device__ __forceinline__ void forward_epilogue(const SplitFwdArgs &p, uint32_t
     for (int j = 0; j < HALF / SEG; ++j) {
         f32x2 za[4], zx[4], la[4], lx[4];
         const int tb = t0 + j * SEG;
+        __syncwarp();   // lanes part in a walk (below), and in loads of tokens that may not exist
         tmem_ld8p(tm + j * SEG, za); tmem_ld8p(tm + TOK + j * SEG, la); tmem_ld8p(tm + 2 * TOK + j * SEG, zx); tmem_ld8p(tm + 3 * TOK + j * SEG, lx);
         float xs[SEG];
         if (SAVE && j > 0) fetch(tb);
@@ -370,7 +373,7 @@ __device__ __forceinline__ void forward_epilogue(const SplitFwdArgs &p, uint32_t
         }
         const size_t e = ((size_t)b * T + tb) * D + d;
         walk_segment<SAVE, POLY>(k, za, zx, xs, tb, T, D, cv, SAVE ? f.save_r + e : nullptr, SAVE ? f.save_i + e : nullptr);
-        if (!SAVE) { tmem_st8p(tm + j * SEG, za); tmem_st8p(tm + 2 * TOK + j * SEG, zx); }
+        if (!SAVE) { __syncwarp(); tmem_st8p(tm + j * SEG, za); tmem_st8p(tm + 2 * TOK + j * SEG, zx); }
     }
     if (!SAVE) tmem_st_wait();
     float P = k.P, h = k.h;

@@ -60,7 +60,7 @@ def test_the_reader_sees_what_it_should():
     assert reached_apart("for (;;) { tmem_ld16(a, x); if (last) f(); }") == []
 
 
-@pytest.mark.parametrize("name", ["rglru_sm100_linattn.cu", "rglru_sm100_linear.cu"])
+@pytest.mark.parametrize("name", sorted(f for f in os.listdir(CSRC) if f.startswith("rglru_sm100")))
 def test_tensor_memory_is_read_by_whole_warps(name):
     assert reached_apart(source(name)) == []
 
