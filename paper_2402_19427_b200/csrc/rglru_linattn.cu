@@ -361,9 +361,11 @@ bool clear_of(const MixTensor &a, size_t a_bytes, long long row_a, const MixTens
     if (!overlap(a.p, a_bytes, b.p, b_bytes)) return true;
     if ((uintptr_t)a.p > (uintptr_t)b.p) return clear_of(b, b_bytes, row_b, a, a_bytes, row_a, s);
     if ((s->T > 1 && a.token != b.token) || (s->B > 1 && a.batch != b.batch)) return false;
-    const long long token = s->T > 1 ? a.token : LLONG_MAX, batch = s->B > 1 ? a.batch : LLONG_MAX, inner = token < batch ? token : batch;
+    const long long token = s->T > 1 ? a.token : LLONG_MAX, batch = s->B > 1 ? a.batch : LLONG_MAX;
+    const long long inner = token < batch ? token : batch, outer = token < batch ? batch : token, rows = token < batch ? s->T : s->B;   // rows: of a run `inner` apart
     const long long off = (long long)(((uintptr_t)b.p - (uintptr_t)a.p) / io_bytes(s->io));
-    return off >= row_a && off <= inner - row_b;
+    if (off < row_a || off > inner - row_b) return false;
+    return outer == LLONG_MAX || (rows - 1) * inner + off + row_b <= outer;   // b's last row ends before a's next run
 }
 const rglru_linear_attention_strides_t DENSE{};
 size_t state_bytes(const rglru_linear_attention_shape_t *s) { return (size_t)s->B * s->H * s->dk * s->dv * sizeof(float); }

@@ -166,3 +166,23 @@ def test_gradients_side_by_side(b):
     for name, token in (("dq", 320), ("dk", 320), ("dv", 640)):
         getattr(other, name)[0], getattr(other, name)[1] = token, 32 * token
     assert bwd(0, 256, 512, big, other) == b.ERR_ALIAS
+
+
+def test_gradients_side_by_side_in_sequences_without_a_gap(b):
+    """A sequence's last token row and the next sequence's first may not share bytes either, when the distance between sequences is no multiple
+    of the one between tokens"""
+    lib, S, St = b.load(), b.LinearAttentionShape, b.LinearAttentionStrides
+    B, T = 2, 16
+    shape = S(B, T, 2, 64, 32, b.BF16, 0.125, 0)
+
+    def bwd(token, batch, offsets):
+        st = St()
+        for name in ("dq", "dk", "dv"):
+            getattr(st, name)[0], getattr(st, name)[1] = token, batch
+        return lib.rglru_linear_attention_backward(ctypes.byref(shape), ctypes.byref(st), at(0), at(1), at(2), at(3), at(4), at(5), at(6),
+                                                   *(at(7, 2 * o) for o in offsets), at(10), at(11), 1 << 30, None)
+
+    # rows of 128 (dq), 128 (dk) and 64 (dv) elements, 320 from row to row; the outer distance ends behind the first of them
+    for outer_of in ((lambda n: (320, (n - 1) * 320 + 128)), (lambda n: ((n - 1) * 320 + 128, 320))):   # [B,T,...] and [T,B,...]
+        inner = T if outer_of(2)[0] == 320 else B
+        assert bwd(*outer_of(inner), (0, 128, 256)) == b.ERR_ALIAS
