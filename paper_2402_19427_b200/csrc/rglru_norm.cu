@@ -559,7 +559,7 @@ int32_t rglru_layer_norm(const rglru_norm_shape_t *s, const void *x, const float
 
 size_t rglru_layer_norm_workspace_bytes(const rglru_norm_shape_t *s) {
     if (check_norm(s) != RGLRU_OK) return 0;
-    return up256((size_t)backward_blocks(s, norm_layout(s->N, s->io, true)) * 2 * s->N * sizeof(float));
+    return WS_HEADER_BYTES + up256((size_t)backward_blocks(s, norm_layout(s->N, s->io, true)) * 2 * s->N * sizeof(float));
 }
 
 int32_t rglru_layer_norm_backward(const rglru_norm_shape_t *s, const void *dy, const void *x, const float *mean, const float *rstd, const float *weight,
@@ -577,7 +577,7 @@ int32_t rglru_layer_norm_backward(const rglru_norm_shape_t *s, const void *dy, c
     const Layout l = norm_layout(s->N, s->io, true);
     NormArgs a = norm_args(s, l);
     a.x = x; a.dy = dy; a.weight = weight; a.mean_in = mean; a.rstd_in = rstd; a.out = dx;
-    a.part = sums ? (float *)workspace : nullptr;
+    a.part = sums ? (float *)((char *)workspace + WS_HEADER_BYTES) : nullptr;
     const int blocks = backward_blocks(s, l);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     const bool f32 = s->io == RGLRU_F32;

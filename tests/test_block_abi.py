@@ -186,3 +186,8 @@ def test_gradients_side_by_side_in_sequences_without_a_gap(b):
     for outer_of in ((lambda n: (320, (n - 1) * 320 + 128)), (lambda n: ((n - 1) * 320 + 128, 320))):   # [B,T,...] and [T,B,...]
         inner = T if outer_of(2)[0] == 320 else B
         assert bwd(*outer_of(inner), (0, 128, 256)) == b.ERR_ALIAS
+
+
+def test_every_workspace_has_room_for_the_status(b):
+    """256 bytes in front of what a call puts there: the partial sums of the norm's gradients [blocks][2][N] fp32 (one row: one block)"""
+    assert b.load().rglru_layer_norm_workspace_bytes(ctypes.byref(b.NormShape(1, 64, b.BF16, 1, 0.0))) == 256 + 2 * 64 * 4
