@@ -45,6 +45,7 @@ struct GemmArgs {
     int wide;                             // bytes a thread may store at once along N (32, 16, or 0: one value)
     LinearEpilogue e;
     float *part;                          // [tile - whole][split][256 x NT] fp32, along the results' innermost dimension
+    float *carry;                         // [CTA][NT][128] fp32: what a tile's earlier accumulators held (bf16, long K), or null
     uint32_t *status;
     unsigned long long spin_ns;
 };
@@ -157,10 +158,13 @@ template <typename IO> __device__ __forceinline__ void finish_column(const GemmA
     }
 }
 
-// fp32 io: accumulators are emptied into registers every DRAIN_BLOCKS K blocks (NT <= 128); bf16: a tile's sum stays in tensor memory.
-constexpr int DRAIN_BLOCKS = 4;
+// The tensor core cuts off what does not fit the sum so far, so an accumulator takes a limited number of terms.  fp32 io: it is emptied into registers every
+// DRAIN_BLOCKS K blocks (NT <= 128).  bf16: 16384 terms (some 2^-13 of the sum at worst, a sixteenth of the result's own half step), then its sum goes
+// on in fp32 in the block's place in `carry`, which a thread writes and reads back alone: 128 KB a CTA, out of L2, every 256 K blocks.
+constexpr int DRAIN_BLOCKS = 4, LONG_BLOCKS = 256;
 template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm_kernel(const __grid_constant__ GemmArgs p) {
     constexpr bool DRAIN = sizeof(IO) == 4;
+    constexpr int TAKE = DRAIN ? DRAIN_BLOCKS : LONG_BLOCKS;   // K blocks of an accumulator
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw), base = (raw_addr + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (base - raw_addr);
@@ -242,7 +246,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
             for (int t = pair; t < ntiles && ok; t += npairs) {
                 const Tile tl = tile_at(t);
                 for (int v = tl.v0; v < tl.v1 && ok; ++v) {
-                    const int within = DRAIN ? (v - tl.v0) % DRAIN_BLOCKS : v - tl.v0, acc = it & 1;
+                    const int within = (v - tl.v0) % TAKE, acc = it & 1;
                     if (within == 0) ok = mbar_wait_spin(BAR_ACCEMPTY(acc), ((it >> 1) & 1) ^ 1, spin, abort_flag);
                     ok = ok && mbar_wait_spin(BAR_FULL(s), turn, spin, abort_flag);
                     if (!ok) break;
@@ -253,7 +257,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
 #pragma unroll
                     for (int k = 1; k < 4; ++k) mma_ss2(d, da + k * a_step, db + k * b_step, idesc, 1);
                     tc_commit2(BAR_EMPTY(s), 3);
-                    if (v + 1 == tl.v1 || (DRAIN && within + 1 == DRAIN_BLOCKS)) { tc_commit2(BAR_ACCFULL(acc), 3); ++it; }
+                    if (v + 1 == tl.v1 || within + 1 == TAKE) { tc_commit2(BAR_ACCFULL(acc), 3); ++it; }
                     if (++s == stages) { s = 0; turn ^= 1; }
                 }
             }
@@ -314,25 +318,37 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
                 for (int j = 0; j < 2; ++j)
                     if (half * 32 + j * 64 < p.NT) finish(tl.n + half * 32 + j * 64, sum[j]);
             } else {
-                const int acc = it & 1;
-                ok = warp_wait_cl(BAR_ACCFULL(acc), (it >> 1) & 1, spin, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
+                float *carry = p.carry + (size_t)blockIdx.x * p.NT * 128 + q * 32 + lane;
+                for (int v0 = tl.v0; v0 < tl.v1 && ok; v0 += TAKE, ++it) {
+                    const int acc = it & 1;
+                    ok = warp_wait_cl(BAR_ACCFULL(acc), (it >> 1) & 1, spin, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
 #pragma unroll 1
-                for (int c = half * 32; c < p.NT; c += 64) {
-                    f32x2 x[16];
-                    __syncwarp();   // lanes part at rows that do not exist below, and tensor memory is read by whole warps
-                    tmem_ld32(lanes + acc * 256 + c, x);
-                    tmem_ld_wait();
-                    float v[32];
+                    for (int c = half * 32; c < p.NT; c += 64) {
+                        f32x2 x[16];
+                        __syncwarp();   // lanes part at rows that do not exist below, and tensor memory is read by whole warps
+                        tmem_ld32(lanes + acc * 256 + c, x);
+                        tmem_ld_wait();
+                        float v[32];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) { v[2 * i] = x[i].x; v[2 * i + 1] = x[i].y; }
-                    finish(tl.n + c, v);
+                        for (int i = 0; i < 16; ++i) { v[2 * i] = x[i].x; v[2 * i + 1] = x[i].y; }
+                        if (v0 != tl.v0) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] += carry[(c + j) * 128];
+                        }
+                        if (v0 + TAKE < tl.v1) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) carry[(c + j) * 128] = v[j];
+                        } else {
+                            finish(tl.n + c, v);
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_at(BAR_ACCEMPTY(acc), 0);
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_at(BAR_ACCEMPTY(acc), 0);
-                ++it;
+                if (!ok) break;
             }
         }
         if (!ok && lane == 0) { *abort_flag = 1; atomicExch(p.status, STATUS_MAGIC | (uint32_t)RGLRU_ERR_TIMEOUT); }
@@ -435,7 +451,7 @@ template <typename IO> __global__ void __launch_bounds__(256) linear_pack_kernel
 struct Plan {
     bool swapped, pack_a, pack_b;   // swapped: the caller's B is the kernel's A
     int NT, nx, ny, kblocks, vblocks, whole, splits, per_split;
-    size_t a_bytes, b_bytes, part_bytes;
+    size_t a_bytes, b_bytes, part_bytes, carry_bytes;
 };
 inline bool f32(const LinearProduct &g) { return g.io == RGLRU_F32; }
 size_t packed_bytes(const LinearOperand &o, bool is_f32) {
@@ -473,6 +489,8 @@ Plan make_plan(const LinearProduct &g) {
     p.a_bytes = a.packed ? 0 : packed_bytes(a, f32(g));
     p.b_bytes = b.packed ? 0 : packed_bytes(b, f32(g));
     p.part_bytes = (size_t)((long long)p.nx * p.ny - p.whole) * p.splits * 256 * p.NT * sizeof(float);
+    const int longest = p.whole ? p.vblocks : p.per_split;
+    p.carry_bytes = f32(g) || longest <= LONG_BLOCKS ? 0 : (size_t)2 * PAIRS * 128 * p.NT * sizeof(float);
     return p;
 }
 
@@ -526,7 +544,7 @@ size_t sm100_linear_packed_bytes(const LinearOperand &o, int io) { return packed
 
 size_t sm100_linear_bytes(const LinearProduct &g) {
     const Plan p = make_plan(g);
-    return p.a_bytes + p.b_bytes + p.part_bytes;
+    return p.a_bytes + p.b_bytes + p.part_bytes + p.carry_bytes;
 }
 
 cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status, cudaStream_t st) {
@@ -546,6 +564,10 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
     a.out_m = p.swapped ? 1 : g.N; a.out_n = p.swapped ? g.N : 1;
     a.e = g.e;
     a.part = (float *)(at + p.a_bytes + p.b_bytes);
+    if (p.carry_bytes) {
+        a.carry = (float *)(at + p.a_bytes + p.b_bytes + p.part_bytes);
+        if (pairs > PAIRS) pairs = PAIRS;   // as many as have a place there
+    }
     const int per16 = 16 / (int)io_bytes(g.io);
     a.wide = g.N % per16 != 0 ? 0 : g.N % (2 * per16) == 0 && aligned(g.e.y, 32) && aligned(g.e.preact, 32) ? 32 : 16;
     a.stages = (int)((a.out_n == 1 && !a.wide ? RING - TURN : RING) / (A_BYTES + (uint32_t)p.NT * 64u));

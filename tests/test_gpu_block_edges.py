@@ -29,3 +29,23 @@ def test_a_recorded_timeout_survives_calls_that_share_the_workspace():
         assert binding.query_status(ws) == binding.ERR_TIMEOUT, name
         call()
         assert binding.query_status(ws) == binding.OK, name
+
+
+@pytest.mark.parametrize("product", ["forward", "dweight"])
+def test_sums_over_many_terms_are_as_exact_as_fp32(product):
+    """All terms of one sign, half a million of them: an accumulator that adds up by cutting off must not take them all."""
+    from paper_2402_19427_b200 import binding
+    terms, rows, cols = 1 << 19, 2560, 2048   # 80 tiles of 256 x 256: most of them are one CTA pair's, with all of their terms
+    g = torch.Generator(device="cuda").manual_seed(5)
+    a = (0.5 + torch.rand(terms, rows, generator=g, device="cuda", dtype=torch.bfloat16)) * (1 + torch.rand(rows, generator=g, device="cuda")).bfloat16()
+    b = 0.5 + torch.rand(terms, cols, generator=g, device="cuda", dtype=torch.bfloat16)
+    if product == "dweight":
+        got = binding.linear_backward(a, b, torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16), need=("weight",))["weight"]
+    else:
+        got = binding.linear(a.T.contiguous(), b.T.contiguous())
+    for m in (0, 1024, rows - 64):
+        ref = a[:, m:m + 64].double().T @ b[:, :64].double()
+        # 16384 terms an accumulator, 16 an instruction, each of which cuts off less than two steps of the sum (2^-23 relative); the
+        # accumulators' sum takes 32 roundings.  Then one rounding to bf16: half a step of the result's own binade
+        half = torch.exp2(torch.floor(torch.log2(ref)) - 8)
+        bo.assert_within(product, got[m:m + 64, :64], ref, half + (2 * 1024 * 2 + 32) * bo.U32 * ref)
