@@ -19,7 +19,7 @@ using namespace ptx;
 
 struct NormArgs {
     long long rows;
-    int N, G;            // G: threads a row (narrow rows: 8, 16 or 32; wide ones: the block)
+    int N, G;            // G: threads a row (narrow rows: 4, 8, 16 or 32; wide ones: the block)
     int center;
     float eps, inv_n;
     const void *x, *dy;
@@ -295,7 +295,7 @@ template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __lau
                 if (mine.in[v]) { nx[v] = own16(own + (slot * 2 * V + v) * row_bytes); ny[v] = own16(own + (slot * 2 * V + V + v) * row_bytes); }
         }
         unpack_row<IO, VE, V>(nx, h);
-        unpack_row<IO, VE, V>(ny, g);   // zeros behind the row's end, so nothing of those columns counts in any sum
+        unpack_row<IO, VE, V>(ny, g);   // zeros behind the row's end
         fetch(slot, row + (RING ? AHEAD : 1) * groups);
         slot = slot + 1 == AHEAD ? 0 : slot + 1;
         fetch_statistics(row + groups);
@@ -308,7 +308,7 @@ template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __lau
                 db[i] = add2(g[i], db[i]);
             }
             g[i] = mul2(g[i], w[i]);
-            s0 = fma2(g[i], h[i], s0);
+            if (mine.pair_in(i)) s0 = fma2(g[i], mine.masked(i, h[i]), s0);   // behind the row's end h is -mu r, which may be infinite
             s1 = add2(g[i], s1);
         }
         float s[2] = {s0.x + s0.y, s1.x + s1.y};

@@ -49,3 +49,19 @@ def test_sums_over_many_terms_are_as_exact_as_fp32(product):
         # accumulators' sum takes 32 roundings.  Then one rounding to bf16: half a step of the result's own binade
         half = torch.exp2(torch.floor(torch.log2(ref)) - 8)
         bo.assert_within(product, got[m:m + 64, :64], ref, half + (2 * 1024 * 2 + 32) * bo.U32 * ref)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 4, 5, 12, 264, 2565])
+def test_norm_of_large_means_and_widths_that_leave_threads_idle(N, io):
+    """Rows of one large value, (0 - mean) r beyond fp32's range: what lies behind a row's end takes no part"""
+    from paper_2402_19427_b200 import binding
+    x = torch.full((9, N), 2.0 ** 122, device="cuda", dtype=DT[io])
+    g = torch.Generator(device="cuda").manual_seed(N)
+    dy, w = torch.randn(9, N, generator=g, device="cuda").to(DT[io]), 1 + 0.1 * torch.randn(N, generator=g, device="cuda")
+    mean, rstd = torch.full((9,), 2.0 ** 122, device="cuda"), torch.full((9,), 300.0, device="cuda")
+    got = binding.layer_norm_backward(dy, x, rstd, mean=mean, weight=w)
+    ref = bo.norm_backward(dy, x, mean, rstd, w, True)
+    bo.assert_within("dx", got["x"], ref[0], 80 * bo.U32 * ref[3] + bo.half_step(DT[io]) * ref[0].abs())
+    assert (got["weight"] == 0).all()
+    bo.assert_within("dbias", got["bias"], ref[2], 64 * bo.U32 * ref[5])
