@@ -198,6 +198,7 @@ template <typename IO, int CB, int VEC, bool STATE_ONLY> __global__ void __launc
                 if (row + 16 * i >= dk4) continue;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                    if (row + 16 * i + e >= dk) continue;   // padding stays 0: out of an infinite v it would become NaN, and q's padding bring that into the outputs
                     float4 *at_row = (float4 *)&S[(row + 16 * i + e) * NC + col];
                     const float4 o = *at_row;
                     const f32x2 *z = sum[i][e / 2];

@@ -65,3 +65,21 @@ def test_norm_of_large_means_and_widths_that_leave_threads_idle(N, io):
     bo.assert_within("dx", got["x"], ref[0], 80 * bo.U32 * ref[3] + bo.half_step(DT[io]) * ref[0].abs())
     assert (got["weight"] == 0).all()
     bo.assert_within("dbias", got["bias"], ref[2], 64 * bo.U32 * ref[5])
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("dk", [5, 8, 33])
+def test_an_infinite_value_of_v_is_infinite_in_later_outputs(dk, io):
+    """Widths that no tensor-core kernel takes: an infinity in v is one in its column from its token on, also where dk is no multiple of four"""
+    from paper_2402_19427_b200 import binding
+    T, dv, at, col = 150, 6, 3, 2
+    g = torch.Generator(device="cuda").manual_seed(dk)
+    q, k, v = ((0.5 + torch.rand(1, T, 2, w, generator=g, device="cuda")).to(DT[io]) for w in (dk, dk, dv))
+    ld = torch.tensor([-0.01, -0.1], device="cuda")
+    clean, s = binding.linear_attention_prefill(q, k, v, ld)
+    v = v.clone(); v[0, at, 1, col] = float("inf")
+    o, sT = binding.linear_attention_prefill(q, k, v, ld)
+    assert torch.isposinf(o[0, at:, 1, col]).all() and torch.isposinf(sT[0, 1, :, col]).all()
+    o[0, at:, 1, col] = clean[0, at:, 1, col]
+    sT[0, 1, :, col] = s[0, 1, :, col]
+    assert torch.equal(o, clean) and torch.equal(sT, s)
