@@ -321,7 +321,7 @@ int32_t rglru_layer_norm_backward(const rglru_norm_shape_t *shape, const void *d
 typedef enum { RGLRU_ACT_NONE = 0, RGLRU_ACT_GELU = 1, RGLRU_ACT_SILU = 2 } rglru_activation_t;
 typedef struct {
     int64_t M;       /* rows (tokens), up to 2^31 - 1 */
-    int32_t K, N;    /* inputs and outputs of a row */
+    int32_t K, N;    /* inputs and outputs of a row, up to 2^31 - 1024 */
     int32_t io;      /* rglru_dtype_t */
     int32_t activation;
     uint32_t flags;
@@ -376,7 +376,7 @@ int32_t rglru_linear_attention_prefill(const rglru_linear_attention_shape_t *sha
 
 /*
  * One token for each of B sequences: q, k [B,H,dk], v, o [B,H,dv] io, dense; s [B,H,dk,dv] fp32 updated in place.  o must not overlap
- * q, k or v.  Any dk and dv.
+ * q, k or v.  dk up to 4096, dv up to 2^31 - 1024.
  */
 int32_t rglru_linear_attention_decode_step(const rglru_linear_attention_shape_t *shape, const void *q, const void *k, const void *v,
                                            const float *log_decay, float *s, void *o, void *cuda_stream);

@@ -13,6 +13,7 @@ namespace {
 using namespace ptx;
 
 constexpr int MAX_WIDTH = 256;
+constexpr int MAX_STEP_DK = 4096, MAX_STEP_DV = INT_MAX - 1023;   // of the token step: q and k in shared memory; a block's last column, behind the row's end, still is an int
 constexpr int C = 32, GEN_THREADS = 256;   // tokens a chunk
 
 template <typename IO> __device__ __forceinline__ float at(const void *p, long long i) {
@@ -341,7 +342,7 @@ int32_t check_mix(const rglru_linear_attention_shape_t *s, bool need_T) {
     if (s == nullptr) return RGLRU_ERR_NULL;
     if (s->B <= 0 || s->H <= 0 || s->dk <= 0 || s->dv <= 0 || (need_T && s->T <= 0) || !isfinite(s->scale)) return RGLRU_ERR_SHAPE;
     if (s->io != RGLRU_F32 && s->io != RGLRU_BF16) return RGLRU_ERR_UNSUPPORTED;
-    if (need_T ? s->dk > MAX_WIDTH || s->dv > MAX_WIDTH : s->dk > 4096) return RGLRU_ERR_UNSUPPORTED;
+    if (need_T ? s->dk > MAX_WIDTH || s->dv > MAX_WIDTH : s->dk > MAX_STEP_DK || s->dv > MAX_STEP_DV) return RGLRU_ERR_UNSUPPORTED;
     if ((long long)s->B * s->H > INT32_MAX / 4 || (need_T && s->T > (1 << 30))) return RGLRU_ERR_UNSUPPORTED;
     return RGLRU_OK;
 }

@@ -283,7 +283,7 @@ size_t product_bytes(const rglru_linear_shape_t *s, const LinearProduct &g) { re
 // 2560 5.0 and 8.3 us), more up to 2^25 products (4 x 2560 x 2560 9.9 and 10.2, 6 rows 17 and 10; 8 x 512 x 1024 4.8 and 6.6)
 bool is_few_rows(const rglru_linear_shape_t *s) {
     if (forced_generic(s) || s->M > FEW_ROWS) return false;
-    return s->io == RGLRU_F32 || s->M == 1 || s->M * s->K * (long long)s->N <= 1 << 25;
+    return s->io == RGLRU_F32 || s->M == 1 || (double)s->M * s->K * s->N <= 1 << 25;
 }
 cudaError_t run_product(const rglru_linear_shape_t *s, const LinearProduct &g, void *scratch, void *workspace, cudaStream_t st) {
     if (!forced_generic(s)) return sm100_linear(g, scratch, (uint32_t *)workspace, st);
@@ -292,9 +292,10 @@ cudaError_t run_product(const rglru_linear_shape_t *s, const LinearProduct &g, v
     return generic_gemm(GenericGemm{g.a.p, g.b.p, by_row(g.a), by_k(g.a), by_row(g.b), by_k(g.b), g.M, g.N, g.K, g.e}, g.io, st);
 }
 
+constexpr int MAX_COLUMNS = INT32_MAX - 1023;   // a block's last column, behind the row's end, still is an int
 int32_t check_linear(const rglru_linear_shape_t *s) {
     if (s == nullptr) return RGLRU_ERR_NULL;
-    if (s->M <= 0 || s->M > INT32_MAX || s->K <= 0 || s->N <= 0) return RGLRU_ERR_SHAPE;
+    if (s->M <= 0 || s->M > INT32_MAX || s->K <= 0 || s->N <= 0 || s->K > MAX_COLUMNS || s->N > MAX_COLUMNS) return RGLRU_ERR_SHAPE;
     if (s->io != RGLRU_F32 && s->io != RGLRU_BF16) return RGLRU_ERR_UNSUPPORTED;
     if (s->activation < RGLRU_ACT_NONE || s->activation > RGLRU_ACT_SILU) return RGLRU_ERR_UNSUPPORTED;
     return RGLRU_OK;

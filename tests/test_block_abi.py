@@ -191,3 +191,15 @@ def test_gradients_side_by_side_in_sequences_without_a_gap(b):
 def test_every_workspace_has_room_for_the_status(b):
     """256 bytes in front of what a call puts there: the partial sums of the norm's gradients [blocks][2][N] fp32 (one row: one block)"""
     assert b.load().rglru_layer_norm_workspace_bytes(ctypes.byref(b.NormShape(1, 64, b.BF16, 1, 0.0))) == 256 + 2 * 64 * 4
+
+
+def test_sizes_behind_which_indices_would_not_fit(b):
+    """A row of nearly 2^31 elements fits the memory, but not the kernels' 32-bit columns: refused, as the header says"""
+    lib, big, r = b.load(), (1 << 31) - 1016, ctypes.byref
+    assert lib.rglru_linear(r(b.LinearShape(1, 8, big, b.BF16, 0, 0)), at(0), at(1), None, None, at(2), None, at(3), 1 << 40, None) == b.ERR_SHAPE
+    assert lib.rglru_linear_backward(r(b.LinearShape(1, 8, big, b.BF16, 0, 0)), at(0), at(1), at(2), None, None, None, at(3), at(4), 1 << 40, None) == b.ERR_SHAPE
+    assert lib.rglru_linear(r(b.LinearShape(1, big, 8, b.BF16, 0, 0)), at(0), at(1), None, None, at(2), None, at(3), 1 << 40, None) == b.ERR_SHAPE
+    assert lib.rglru_linear_attention_decode_step(r(b.LinearAttentionShape(1, 0, 1, 1, big, b.F32, 1.0, 0)), at(0), at(1), at(2), at(3), at(4), at(5 + 4), None) == b.ERR_UNSUPPORTED
+    assert lib.rglru_linear_attention_decode_step(r(b.LinearAttentionShape(1, 0, 1, 4104, 8, b.F32, 1.0, 0)), at(0), at(1), at(2), at(3), at(4), at(5), None) == b.ERR_UNSUPPORTED
+    # sizes are computed without overflow up to there
+    assert lib.rglru_linear_workspace_bytes(r(b.LinearShape(8, 1 << 30, 1 << 30, b.F32, 0, 0)), b.OP_PREFILL) == 256
