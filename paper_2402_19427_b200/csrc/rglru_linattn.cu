@@ -286,7 +286,7 @@ struct StepArgs {
     void *o;
 };
 template <typename IO, int VE, int LPR> __global__ void __launch_bounds__(256) mix_step_kernel(StepArgs a) {
-    extern __shared__ float sm[];     // q, k [dk], then [256][VE] shares of o
+    extern __shared__ __align__(16) float sm[];     // q, k [dk], then [256][VE] shares of o
     constexpr int RG = 256 / LPR, UNROLL = 8;
     dependency_wait();
     const int slices = (a.dv + LPR * VE - 1) / (LPR * VE), slice = blockIdx.x % slices;

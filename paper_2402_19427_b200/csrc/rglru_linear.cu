@@ -29,7 +29,7 @@ template <typename IO> __device__ __forceinline__ void put(void *p, long long i,
     else ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
 }
 template <typename IO> __global__ void __launch_bounds__(256) generic_linear_kernel(GenericGemm g) {
-    __shared__ float sa[GK][GT + 4], sb[GK][GT + 4];
+    __shared__ __align__(16) float sa[GK][GT + 4], sb[GK][GT + 4];
     dependency_wait();
     const long long tiles_n = (g.N + GT - 1) / GT, m0 = blockIdx.x / tiles_n * GT, n0 = blockIdx.x % tiles_n * GT;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
@@ -85,7 +85,7 @@ template <typename IO> __global__ void __launch_bounds__(256) generic_linear_ker
 // Tensor cores would need the weights in shared memory first, the tokens padded and K split over the SMs by a launch of its own.
 constexpr int FEW_OUT = 4;
 template <typename IO, int VE, int MT> __global__ void __launch_bounds__(256) few_rows_kernel(GenericGemm g) {
-    __shared__ float red[8][FEW_OUT * MT];
+    __shared__ __align__(16) float red[8][FEW_OUT * MT];
     using Vec = LinearVec<IO, VE>;
     constexpr int PAIRS = VE > 1 ? VE / 2 : 1;
     dependency_wait();
@@ -164,7 +164,7 @@ struct DzArgs {
     float *part;              // [row blocks][N] or null
 };
 template <typename IO, int VE> __global__ void __launch_bounds__(256, 2) linear_dz_kernel(DzArgs a) {
-    __shared__ float red[8][32 * VE];
+    __shared__ __align__(16) float red[8][32 * VE];
     dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = (blockIdx.x * 32 + lane) * VE;

@@ -166,7 +166,7 @@ __device__ __forceinline__ f32x2 both(float x) { return pack2(x, x); }
 // Rows of at most G V VE elements.  Thread t of a group holds the vectors t, t + G, ... of its row, the weights of its columns, and its next
 // row's vectors on their way.  327680 x 128 bf16: 30 us for 168 MB, 86 % of the copy rate; 16384 x 4096: 47 us for 268 MB.
 template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_kernel(NormArgs a) {
-    __shared__ float red[2][1][16];
+    __shared__ __align__(16) float red[2][1][16];
     constexpr int PAIRS = VE * V / 2;
     if (WIDE && threadIdx.x < 32) red[threadIdx.x >> 4][0][threadIdx.x & 15] = 0.0f;
     dependency_wait();
@@ -239,8 +239,8 @@ constexpr int AHEAD = 3;   // rows that a wide row's threads have on their way i
 // The gradients, rows as above.  The column sums of a group's rows stay in registers and leave once, added over the block's groups.  16384 x 4096
 // bf16: 76 us for 403 MB, 79 % of the copy rate; dx alone 71.
 template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __launch_bounds__(MAXT) norm_backward_kernel(NormArgs a) {
-    __shared__ float red[2][2][16];
-    extern __shared__ float cols[];   // narrow rows: [2][N] sums of the block
+    __shared__ __align__(16) float red[2][2][16];
+    extern __shared__ __align__(16) float cols[];   // narrow rows: [2][N] sums of the block
     constexpr int PAIRS = VE * V / 2;
     if (WIDE && threadIdx.x < 32) { red[threadIdx.x >> 4][0][threadIdx.x & 15] = 0.0f; red[threadIdx.x >> 4][1][threadIdx.x & 15] = 0.0f; }
     dependency_wait();
@@ -356,7 +356,7 @@ template <typename IO, int VE, int V, bool WIDE, int MAXT> __global__ void __lau
 
 // dweight | dbias = the sums of the blocks' columns: a block of 32 warps for 32 columns, every warp a 32nd of the parts, added up in a fixed order
 __global__ void __launch_bounds__(1024) norm_columns_kernel(const float *part, int parts, int N, float *dweight, float *dbias) {
-    __shared__ float red[32][33];
+    __shared__ __align__(16) float red[32][33];
     dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long c = (long long)blockIdx.x * 32 + lane, stride = 2ll * N;
@@ -388,7 +388,7 @@ template <typename IO> __device__ __forceinline__ void put(void *p, long long i,
     store_vec<IO, 1>((IO *)p + i, f);
 }
 template <typename IO> __global__ void __launch_bounds__(512) norm_long_kernel(NormArgs a) {
-    __shared__ float red[2][1][16];
+    __shared__ __align__(16) float red[2][1][16];
     dependency_wait();
     GroupSum<true, 1> sum{red};
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -413,7 +413,7 @@ template <typename IO> __global__ void __launch_bounds__(512) norm_long_kernel(N
     dependency_trigger();
 }
 template <typename IO> __global__ void __launch_bounds__(512) norm_long_backward_kernel(NormArgs a) {
-    __shared__ float red[2][2][16];
+    __shared__ __align__(16) float red[2][2][16];
     dependency_wait();
     GroupSum<true, 2> sum{red};
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {

@@ -108,3 +108,10 @@ def test_register_budgets_are_set_by_whole_warpgroups():
         assert ran and len(ran) % 4 == 0 and all(ran[i] == ran[0] + i for i in range(len(ran))) and ran[0] % 4 == 0, (text[:m.start()].count("\n") + 1, ran)
         seen += ran
     assert sorted(seen) == list(range(warps))
+
+
+@pytest.mark.parametrize("name", ["rglru_norm.cu", "rglru_linear.cu", "rglru_linattn.cu", "rglru_sm100_linear.cu", "rglru_sm100_linattn.cu"])
+def test_shared_arrays_that_are_read_16_bytes_at_a_time_are_aligned(name):
+    """A shared array of floats starts at a multiple of four bytes unless it says more"""
+    text = source(name)
+    assert [m.group() for m in re.finditer(r"__shared__ float \w+", text)] == []
