@@ -268,7 +268,8 @@ int32_t rglru_query_status(void *workspace, void *cuda_stream);
  * the top of this file hold: dense row-major device tensors owned by the caller, fp32 per-channel vectors, sums and
  * statistics in fp32, asynchronous on `cuda_stream`, errors as return codes, capturable.  Every kernel waits for the work before it
  * on the stream before it reads or writes global memory.  A workspace may hold anything when a call starts; calls that may run at the same time need
- * one each (two captured graphs that are replayed in turn may share one).
+ * one each (two captured graphs that are replayed in turn may share one).  No output may overlap another output or an
+ * input, unless its description allows it.
  */
 
 /*

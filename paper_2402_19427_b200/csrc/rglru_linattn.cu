@@ -427,8 +427,8 @@ int32_t rglru_linear_attention_prefill(const rglru_linear_attention_shape_t *s, 
     if (!place(q, st.q, s, s->dk, r.q, nq) || !place(k, st.k, s, s->dk, r.k, nk) || !place(v, st.v, s, s->dv, r.v, nv) || !place(o, st.o, s, s->dv, r.o, no))
         return RGLRU_ERR_SHAPE;
     if (workspace_bytes < rglru_linear_attention_workspace_bytes(s, RGLRU_OP_PREFILL)) return RGLRU_ERR_WORKSPACE;
-    const size_t mat = (size_t)s->B * s->H * s->dk * s->dv * sizeof(float);
-    if (overlap(o, no, q, nq) || overlap(o, no, k, nk) || overlap(o, no, v, nv) || overlap(o, no, s0, mat) || overlap(s_T, mat, q, nq) ||
+    const size_t mat = state_bytes(s), nd = (size_t)s->H * sizeof(float);
+    if (overlap(o, no, log_decay, nd) || overlap(s_T, mat, log_decay, nd) || overlap(o, no, q, nq) || overlap(o, no, k, nk) || overlap(o, no, v, nv) || overlap(o, no, s0, mat) || overlap(s_T, mat, q, nq) ||
         overlap(s_T, mat, k, nk) || overlap(s_T, mat, v, nv) || overlap(s_T, mat, o, no) || (s0 != s_T && overlap(s_T, mat, s0, mat)))
         return RGLRU_ERR_ALIAS;
     a.roles = 1; a.B = s->B; a.T = s->T; a.H = s->H; a.log_decay = log_decay; a.status = (uint32_t *)workspace;
@@ -443,8 +443,8 @@ int32_t rglru_linear_attention_decode_step(const rglru_linear_attention_shape_t 
     if (!q || !k || !v || !log_decay || !state || !o) return RGLRU_ERR_NULL;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(log_decay, 16) || !aligned(state, 16) || !aligned(o, 16)) return RGLRU_ERR_ALIGN;
     const long long units = (long long)s->B * s->H;
-    const size_t io = io_bytes(s->io), nq = units * s->dk * io, nv = units * s->dv * io, ns = (size_t)units * s->dk * s->dv * sizeof(float);
-    if (overlap(o, nv, q, nq) || overlap(o, nv, k, nq) || overlap(o, nv, v, nv) || overlap(o, nv, state, ns) || overlap(state, ns, q, nq) ||
+    const size_t io = io_bytes(s->io), nq = units * s->dk * io, nv = units * s->dv * io, ns = state_bytes(s), nd = (size_t)s->H * sizeof(float);
+    if (overlap(o, nv, log_decay, nd) || overlap(state, ns, log_decay, nd) || overlap(o, nv, q, nq) || overlap(o, nv, k, nq) || overlap(o, nv, v, nv) || overlap(o, nv, state, ns) || overlap(state, ns, q, nq) ||
         overlap(state, ns, k, nq) || overlap(state, ns, v, nv))
         return RGLRU_ERR_ALIAS;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -474,19 +474,19 @@ int32_t rglru_linear_attention_backward(const rglru_linear_attention_shape_t *s,
         return RGLRU_ERR_ALIGN;
     const rglru_linear_attention_strides_t &st = strides ? *strides : DENSE;
     MixTensor t[7];
-    size_t n[9];
+    size_t n[7];
     if (!place(q, st.q, s, s->dk, t[0], n[0]) || !place(k, st.k, s, s->dk, t[1], n[1]) || !place(v, st.v, s, s->dv, t[2], n[2]) ||
         !place(dout, st.o, s, s->dv, t[3], n[3]) || !place(dq, st.dq, s, s->dk, t[4], n[4]) || !place(dk, st.dk, s, s->dk, t[5], n[5]) ||
         !place(dv, st.dv, s, s->dv, t[6], n[6]))
         return RGLRU_ERR_SHAPE;
     if (workspace_bytes < rglru_linear_attention_workspace_bytes(s, RGLRU_OP_BACKWARD)) return RGLRU_ERR_WORKSPACE;
-    const size_t mat = (size_t)s->B * s->H * s->dk * s->dv * sizeof(float);
-    const void *const ins[6] = {q, k, v, dout, s0, ds_T};
-    const size_t in_bytes[6] = {n[0], n[1], n[2], n[3], mat, mat};
+    const size_t mat = state_bytes(s);
+    const void *const ins[7] = {q, k, v, dout, s0, ds_T, log_decay};
+    const size_t in_bytes[7] = {n[0], n[1], n[2], n[3], mat, mat, (size_t)s->H * sizeof(float)};
     void *const outs[4] = {dq, dk, dv, ds0};
     const size_t out_bytes[4] = {n[4], n[5], n[6], mat};
     for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 6; ++j)
+        for (int j = 0; j < 7; ++j)
             if (overlap(outs[i], out_bytes[i], ins[j], in_bytes[j])) return RGLRU_ERR_ALIAS;
     // dq, dk and dv may lie side by side in one gradient of a projection, tokens interleaved
     const long long rk = (long long)s->H * s->dk, rv = (long long)s->H * s->dv;

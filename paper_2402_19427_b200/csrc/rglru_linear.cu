@@ -329,8 +329,8 @@ int32_t rglru_linear(const rglru_linear_shape_t *s, const void *x, const void *w
         !aligned(workspace, 256))
         return RGLRU_ERR_ALIGN;
     if (workspace_bytes < rglru_linear_workspace_bytes(s, RGLRU_OP_PREFILL)) return RGLRU_ERR_WORKSPACE;
-    const size_t io = io_bytes(s->io), xb = (size_t)s->M * s->K * io, wb = (size_t)s->N * s->K * io, yb = (size_t)s->M * s->N * io;
-    if (overlap(y, yb, x, xb) || overlap(y, yb, weight, wb) || (residual != y && overlap(y, yb, residual, yb)) || overlap(preact, yb, x, xb) ||
+    const size_t io = io_bytes(s->io), xb = (size_t)s->M * s->K * io, wb = (size_t)s->N * s->K * io, yb = (size_t)s->M * s->N * io, bb = (size_t)s->N * sizeof(float);
+    if (overlap(y, yb, bias, bb) || overlap(preact, yb, bias, bb) || overlap(y, yb, x, xb) || overlap(y, yb, weight, wb) || (residual != y && overlap(y, yb, residual, yb)) || overlap(preact, yb, x, xb) ||
         overlap(preact, yb, weight, wb) || overlap(preact, yb, residual, yb) || overlap(preact, yb, y, yb))
         return RGLRU_ERR_ALIAS;
     const LinearProduct g = forward_product(s, x, weight, {bias, residual, y, preact, s->activation});

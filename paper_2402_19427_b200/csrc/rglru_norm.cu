@@ -549,7 +549,12 @@ int32_t rglru_layer_norm(const rglru_norm_shape_t *s, const void *x, const float
     if (!x || !y) return RGLRU_ERR_NULL;
     if (!aligned(x, 16) || !aligned(y, 16) || !aligned(weight, 16) || !aligned(bias, 16) || !aligned(mean, 16) || !aligned(rstd, 16)) return RGLRU_ERR_ALIGN;
     const size_t bytes = (size_t)s->rows * s->N * io_bytes(s->io);
-    if (overlap(x, bytes, y, bytes)) return RGLRU_ERR_ALIAS;
+    const size_t vec = (size_t)s->N * sizeof(float), stat = (size_t)s->rows * sizeof(float);
+    if (overlap(x, bytes, y, bytes) || overlap(y, bytes, weight, vec) || overlap(y, bytes, bias, vec) || overlap(y, bytes, mean, stat) || overlap(y, bytes, rstd, stat) ||
+        overlap(mean, stat, rstd, stat))
+        return RGLRU_ERR_ALIAS;
+    for (const float *out : {mean, rstd})
+        if (overlap(out, stat, x, bytes) || overlap(out, stat, weight, vec) || overlap(out, stat, bias, vec)) return RGLRU_ERR_ALIAS;
     const Layout l = norm_layout(s->N, s->io, false);
     NormArgs a = norm_args(s, l);
     a.x = x; a.weight = weight; a.bias = bias; a.out = y; a.mean = mean; a.rstd = rstd;
@@ -573,7 +578,10 @@ int32_t rglru_layer_norm_backward(const rglru_norm_shape_t *s, const void *dy, c
         return RGLRU_ERR_ALIGN;
     if (sums && workspace_bytes < rglru_layer_norm_workspace_bytes(s)) return RGLRU_ERR_WORKSPACE;
     const size_t bytes = (size_t)s->rows * s->N * io_bytes(s->io);
-    if (overlap(dx, bytes, x, bytes) || overlap(dx, bytes, dy, bytes)) return RGLRU_ERR_ALIAS;
+    const size_t vec = (size_t)s->N * sizeof(float), stat = (size_t)s->rows * sizeof(float);
+    if (overlap(dx, bytes, x, bytes) || overlap(dx, bytes, dy, bytes) || (s->center && overlap(dx, bytes, mean, stat)) || overlap(dx, bytes, rstd, stat) ||
+        overlap(dx, bytes, weight, vec) || overlap(dx, bytes, dweight, vec) || overlap(dx, bytes, dbias, vec) || overlap(dweight, vec, dbias, vec))
+        return RGLRU_ERR_ALIAS;
     const Layout l = norm_layout(s->N, s->io, true);
     NormArgs a = norm_args(s, l);
     a.x = x; a.dy = dy; a.weight = weight; a.mean_in = mean; a.rstd_in = rstd; a.out = dx;

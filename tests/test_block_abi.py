@@ -203,3 +203,36 @@ def test_sizes_behind_which_indices_would_not_fit(b):
     assert lib.rglru_linear_attention_decode_step(r(b.LinearAttentionShape(1, 0, 1, 4104, 8, b.F32, 1.0, 0)), at(0), at(1), at(2), at(3), at(4), at(5), None) == b.ERR_UNSUPPORTED
     # sizes are computed without overflow up to there
     assert lib.rglru_linear_workspace_bytes(r(b.LinearShape(8, 1 << 30, 1 << 30, b.F32, 0, 0)), b.OP_PREFILL) == 256
+
+
+def test_outputs_over_vectors(b):
+    """No output may lie over a vector that other blocks still read, or over another output"""
+    lib, r = b.load(), ctypes.byref
+    n = b.NormShape(40, 64, b.BF16, 1, 1e-5)
+
+    def fwd(x=at(0), w=at(1), bias=at(2), y=at(3), mean=at(4), rstd=at(5)):
+        return lib.rglru_layer_norm(r(n), x, w, bias, y, mean, rstd, None)
+
+    for bad in (dict(w=at(3)), dict(bias=at(3, 5104)), dict(mean=at(3)), dict(rstd=at(3, 16)), dict(mean=at(0)), dict(rstd=at(0, 5104)), dict(mean=at(1)), dict(rstd=at(2, 240)),
+                dict(mean=at(5, 144))):
+        assert fwd(**bad) == b.ERR_ALIAS, bad
+
+    def bwd(dy=at(0), x=at(1), mean=at(2), rstd=at(3), w=at(4), dx=at(5), dw=at(6), db=at(7)):
+        return lib.rglru_layer_norm_backward(r(n), dy, x, mean, rstd, w, dx, dw, db, at(8), 1 << 30, None)
+
+    for bad in (dict(mean=at(5)), dict(rstd=at(5, 16)), dict(w=at(5, 5104)), dict(dw=at(5)), dict(db=at(5, 16)), dict(db=at(6, 240))):
+        assert bwd(**bad) == b.ERR_ALIAS, bad
+    lin = b.LinearShape(40, 64, 96, b.BF16, 1, 0)
+
+    def linear(x=at(0), w=at(1), bias=at(2), res=at(3), y=at(4), pre=at(5)):
+        return lib.rglru_linear(r(lin), x, w, bias, res, y, pre, at(6), 1 << 30, None)
+
+    for bad in (dict(bias=at(4)), dict(bias=at(5, 16))):
+        assert linear(**bad) == b.ERR_ALIAS, bad
+    mix = b.LinearAttentionShape(2, 16, 2, 64, 32, b.BF16, 0.125, 0)
+    for o, sT in ((at(3), at(6)), (at(5), at(3))):
+        assert lib.rglru_linear_attention_prefill(r(mix), None, at(0), at(1), at(2), at(3), at(4), o, sT, at(7), 1 << 30, None) == b.ERR_ALIAS
+        assert lib.rglru_linear_attention_decode_step(r(mix), at(0), at(1), at(2), at(3), sT, o, None) == b.ERR_ALIAS
+    for i in range(4):
+        outs = [at(3) if i == j else at(7 + j) for j in range(4)]
+        assert lib.rglru_linear_attention_backward(r(mix), None, at(0), at(1), at(2), at(3), at(4), at(5), at(6), *outs, at(11), 1 << 30, None) == b.ERR_ALIAS
