@@ -73,7 +73,8 @@ typedef enum { RGLRU_OP_PREFILL = 0, RGLRU_OP_DECODE = 1, RGLRU_OP_BACKWARD = 2 
 #define RGLRU_FLAG_FORCE_GENERIC 1u /* use the shape-generic CUDA-core kernels even where a tensor-core kernel exists */
 /* Test hook of the failure path, honoured by rglru_prefill and rglru_backward: blocks that wait for another block's carry
  * record look for a tag that is never published, so the bounded wait (rglru_set_wait_limit_ns) runs out, the kernel drains
- * and returns, and rglru_query_status reports RGLRU_ERR_TIMEOUT.  Outputs are undefined after such a call. */
+ * and returns, and rglru_query_status reports RGLRU_ERR_TIMEOUT.  Outputs are undefined after such a call.  In the tensor-core kernels of
+ * rglru_linear, rglru_linear_attention_prefill and their backwards it is the copies of one operand that never come. */
 #define RGLRU_FLAG_TEST_CARRY_NEVER_ARRIVES 0x40000000u
 
 typedef struct {
@@ -317,7 +318,7 @@ int32_t rglru_layer_norm_backward(const rglru_norm_shape_t *shape, const void *d
  *   y         [M,N] io, out; must not overlap x or weight, nor residual in part
  *   preact    [M,N] io, out or NULL: z, for the backward; must not overlap anything else
  * Sums are fp32; z is rounded only where it is written, y from the unrounded z.  GeLU(v) = v Phi(v), SiLU(v) = v / (1 + exp(-v)).
- * flags: RGLRU_FLAG_NONE or RGLRU_FLAG_FORCE_GENERIC.
+ * flags: RGLRU_FLAG_NONE or RGLRU_FLAG_FORCE_GENERIC (or the test hook).
  */
 typedef enum { RGLRU_ACT_NONE = 0, RGLRU_ACT_GELU = 1, RGLRU_ACT_SILU = 2 } rglru_activation_t;
 typedef struct {

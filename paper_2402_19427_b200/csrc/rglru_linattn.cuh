@@ -30,6 +30,7 @@ struct MixArgs {
     int roles, B, T, H;
     const float *log_decay;
     uint32_t *status;
+    uint32_t flags;           // RGLRU_FLAG_* of the call
 };
 
 // ---- tensor cores (rglru_sm100_linattn.cu): bf16 io, widths that are multiples of 8 up to 128, distances that are multiples of 8

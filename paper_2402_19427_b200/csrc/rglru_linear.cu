@@ -286,7 +286,11 @@ bool is_few_rows(const rglru_linear_shape_t *s) {
     return s->io == RGLRU_F32 || s->M == 1 || (double)s->M * s->K * s->N <= 1 << 25;
 }
 cudaError_t run_product(const rglru_linear_shape_t *s, const LinearProduct &g, void *scratch, void *workspace, cudaStream_t st) {
-    if (!forced_generic(s)) return sm100_linear(g, scratch, (uint32_t *)workspace, st);
+    if (!forced_generic(s)) {
+        LinearProduct p = g;
+        p.flags = s->flags;
+        return sm100_linear(p, scratch, (uint32_t *)workspace, st);
+    }
     auto by_row = [](const LinearOperand &o) { return o.turned ? 1ll : o.cols; };
     auto by_k = [](const LinearOperand &o) { return o.turned ? o.cols : 1ll; };
     return generic_gemm(GenericGemm{g.a.p, g.b.p, by_row(g.a), by_k(g.a), by_row(g.b), by_k(g.b), g.M, g.N, g.K, g.e}, g.io, st);

@@ -32,6 +32,7 @@ struct LinearProduct {
     long long M, N, K;
     int io;
     LinearEpilogue e;
+    uint32_t flags = 0;   // RGLRU_FLAG_* of the call
 };
 // The scratch that the product takes
 size_t sm100_linear_bytes(const LinearProduct &g);

@@ -213,7 +213,7 @@ template <int MODE> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kerne
                     const int k = s & 1;
                     if (!wait(KVE + k, (s >> 1 & 1) ^ 1)) return;
                     load_tile(p, 1, ahead, r.dk, base + SM_K + k * TILE, BAR(KF + k));
-                    load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
+                    if (!(p.m.flags & RGLRU_FLAG_TEST_CARRY_NEVER_ARRIVES)) load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
                     advance<MODE>(ahead, p, s + 1, base + SM_STEPS + 32);
                 };
                 if (steps > 0) load_kv(0);

@@ -48,6 +48,7 @@ struct GemmArgs {
     float *carry;                         // [CTA][NT][128] fp32: what a tile's earlier accumulators held (bf16, long K), or null
     uint32_t *status;
     unsigned long long spin_ns;
+    int b_never_comes;                    // test hook of the waits' limits
 };
 
 // bf16 A and B, fp32 accumulator
@@ -208,7 +209,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
 
     if (warp == 0 || warp == 2) {
         // (a copy takes its thread some 120 cycles: one thread for both operands would be slower than the products of a narrow tile)
-        if (elect_one()) {
+        if (elect_one() && !(warp == 2 && p.b_never_comes)) {
             int s = 0;   // stage of the ring, and its turn
             uint32_t turn = 0;
             const int brows = p.NT / 2;
@@ -571,7 +572,7 @@ cudaError_t sm100_linear(const LinearProduct &g, void *scratch, uint32_t *status
     const int per16 = 16 / (int)io_bytes(g.io);
     a.wide = g.N % per16 != 0 ? 0 : g.N % (2 * per16) == 0 && aligned(g.e.y, 32) && aligned(g.e.preact, 32) ? 32 : 16;
     a.stages = (int)((a.out_n == 1 && !a.wide ? RING - TURN : RING) / (A_BYTES + (uint32_t)p.NT * 64u));
-    a.status = status; a.spin_ns = g_spin_limit_ns;
+    a.status = status; a.spin_ns = g_spin_limit_ns; a.b_never_comes = (g.flags & RGLRU_FLAG_TEST_CARRY_NEVER_ARRIVES) != 0;
     const long long split = (long long)p.nx * p.ny - p.whole, tiles = p.whole + split * p.splits;
     if (tiles > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg{};

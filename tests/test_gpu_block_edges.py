@@ -83,3 +83,44 @@ def test_an_infinite_value_of_v_is_infinite_in_later_outputs(dk, io):
     o[0, at:, 1, col] = clean[0, at:, 1, col]
     sT[0, 1, :, col] = s[0, 1, :, col]
     assert torch.equal(o, clean) and torch.equal(sT, s)
+
+
+@pytest.mark.parametrize("which", ["linear", "linear_split", "linear_few", "linear_f32", "linear_long", "linear_backward", "mix", "mix_cut", "mix_many", "mix_backward"])
+def test_waits_that_run_out_are_reported_and_the_next_call_is_clean(which):
+    """One operand's copies are held back, so that the products wait for them; the limit is a millisecond: the kernels give up, drain and return, the status
+    says so, once, and the next call in the same workspace gives what it gave before."""
+    from paper_2402_19427_b200 import binding
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    ws = torch.zeros(1 << 28, dtype=torch.uint8, device="cuda")
+    if which.startswith("linear"):
+        M, K, N = dict(linear=(2000, 320, 1100), linear_split=(300, 2560, 512), linear_few=(20, 512, 2560), linear_f32=(500, 512, 512), linear_long=(2304, 17000, 2304)).get(which, (700, 512, 640))
+        x, w, dy = rnd(M, K), rnd(N, K), rnd(M, N)
+        if which == "linear_f32":
+            x, w, dy = x.float(), w.float(), dy.float()
+        if which == "linear_backward":
+            call = lambda flags: list(binding.linear_backward(dy, x, w, preact=dy, activation="gelu", flags=flags, workspace=ws).values())  # noqa: E731
+        else:
+            call = lambda flags: [binding.linear(x, w, activation="gelu", residual=dy, flags=flags, workspace=ws)]  # noqa: E731
+    else:
+        B, T, H = dict(mix=(1, 300, 4), mix_cut=(1, 9000, 2), mix_many=(8, 2000, 20)).get(which, (1, 2100, 3))
+        q, k, v, do = (rnd(B, T, H, 64) for _ in range(4))
+        ld = torch.full((H,), -0.01, device="cuda")
+        if which == "mix_backward":
+            call = lambda flags: list(binding.linear_attention_backward(q, k, v, ld, do, state_grads=True, flags=flags, workspace=ws).values())  # noqa: E731
+        else:
+            call = lambda flags: list(binding.linear_attention_prefill(q, k, v, ld, flags=flags, workspace=ws))  # noqa: E731
+    want = call(0)
+    torch.cuda.synchronize()
+    assert binding.query_status(ws) == binding.OK
+    prev = binding.set_wait_limit_ns(1_000_000)
+    try:
+        call(binding.FLAG_TEST_CARRY_NEVER_ARRIVES)
+        torch.cuda.synchronize()
+        assert binding.query_status(ws) == binding.ERR_TIMEOUT
+        assert binding.query_status(ws) == binding.OK
+    finally:
+        binding.set_wait_limit_ns(prev)
+    assert all(torch.equal(a, b) for a, b in zip(call(0), want))
+    torch.cuda.synchronize()
+    assert binding.query_status(ws) == binding.OK
