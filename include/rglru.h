@@ -74,7 +74,7 @@ typedef enum { RGLRU_OP_PREFILL = 0, RGLRU_OP_DECODE = 1, RGLRU_OP_BACKWARD = 2 
 /* Test hook of the failure path, honoured by rglru_prefill and rglru_backward: blocks that wait for another block's carry
  * record look for a tag that is never published, so the bounded wait (rglru_set_wait_limit_ns) runs out, the kernel drains
  * and returns, and rglru_query_status reports RGLRU_ERR_TIMEOUT.  Outputs are undefined after such a call.  In the tensor-core kernels of
- * rglru_linear, rglru_linear_attention_prefill and their backwards it is the copies of one operand that never come. */
+ * rglru_linear, rglru_linear_attention_prefill and their backwards it is the copies of one operand, or of all, that never come. */
 #define RGLRU_FLAG_TEST_CARRY_NEVER_ARRIVES 0x40000000u
 
 typedef struct {

@@ -390,7 +390,7 @@ cudaError_t run_mix(const rglru_linear_attention_shape_t *s, MixArgs &a, void *w
         if (e != cudaSuccess) return e;
         a.role[0].s_in = copy;
     }
-    return may_use_tensor_cores(s) && sm100_mix_supported(a, s->io) ? sm100_mix(a, scratch, st) : generic_mix(a, s->io, (float *)scratch, st);
+    return may_use_tensor_cores(s) && sm100_mix_supported(a, s->io) ? sm100_mix(a, s->flags, scratch, st) : generic_mix(a, s->io, (float *)scratch, st);
 }
 
 }  // namespace
@@ -431,7 +431,7 @@ int32_t rglru_linear_attention_prefill(const rglru_linear_attention_shape_t *s, 
     if (overlap(o, no, log_decay, nd) || overlap(s_T, mat, log_decay, nd) || overlap(o, no, q, nq) || overlap(o, no, k, nk) || overlap(o, no, v, nv) || overlap(o, no, s0, mat) || overlap(s_T, mat, q, nq) ||
         overlap(s_T, mat, k, nk) || overlap(s_T, mat, v, nv) || overlap(s_T, mat, o, no) || (s0 != s_T && overlap(s_T, mat, s0, mat)))
         return RGLRU_ERR_ALIAS;
-    a.roles = 1; a.B = s->B; a.T = s->T; a.H = s->H; a.log_decay = log_decay; a.status = (uint32_t *)workspace; a.flags = s->flags;
+    a.roles = 1; a.B = s->B; a.T = s->T; a.H = s->H; a.log_decay = log_decay; a.status = (uint32_t *)workspace;
     r.dk = s->dk; r.dv = s->dv; r.s_in = s0; r.s_out = s_T; r.first = 1; r.sp = r.si = s->scale; r.su = 1.0f;
     return call_status(run_mix(s, a, workspace, (cudaStream_t)cuda_stream));
 }
@@ -492,7 +492,7 @@ int32_t rglru_linear_attention_backward(const rglru_linear_attention_shape_t *s,
     const long long rk = (long long)s->H * s->dk, rv = (long long)s->H * s->dv;
     if (!clear_of(t[4], n[4], rk, t[5], n[5], rk, s) || !clear_of(t[4], n[4], rk, t[6], n[6], rv, s) || !clear_of(t[5], n[5], rk, t[6], n[6], rv, s) || overlap(ds0, mat, dq, n[4]) || overlap(ds0, mat, dk, n[5]) || overlap(ds0, mat, dv, n[6])) return RGLRU_ERR_ALIAS;
     MixArgs a{};
-    a.roles = 3; a.B = s->B; a.T = s->T; a.H = s->H; a.log_decay = log_decay; a.status = (uint32_t *)workspace; a.flags = s->flags;
+    a.roles = 3; a.B = s->B; a.T = s->T; a.H = s->H; a.log_decay = log_decay; a.status = (uint32_t *)workspace;
     a.role[0] = MixRole{t[3], t[2], t[1], t[4], s->dv, s->dk, s0, nullptr, 1, 0, 1, s->scale, s->scale, 1.0f};
     a.role[1] = MixRole{t[2], t[3], t[0], t[5], s->dv, s->dk, ds_T, nullptr, 1, 1, 0, s->scale, 1.0f, s->scale};
     a.role[2] = MixRole{t[1], t[0], t[3], t[6], s->dk, s->dv, ds_T, ds0, 0, 1, 0, s->scale, 1.0f, s->scale};

@@ -30,13 +30,12 @@ struct MixArgs {
     int roles, B, T, H;
     const float *log_decay;
     uint32_t *status;
-    uint32_t flags;           // RGLRU_FLAG_* of the call
 };
 
 // ---- tensor cores (rglru_sm100_linattn.cu): bf16 io, widths that are multiples of 8 up to 128, distances that are multiples of 8
 bool sm100_mix_supported(const MixArgs &a, int io);
 size_t sm100_mix_bytes(int roles, int B, int T, int H);
-cudaError_t sm100_mix(const MixArgs &a, void *scratch, cudaStream_t st);
+cudaError_t sm100_mix(const MixArgs &a, uint32_t flags, void *scratch, cudaStream_t st);
 
 // decay^n; n = 0 is 1 whatever the decay (log_decay may be minus infinity)
 __device__ __forceinline__ float decay_power(float log_decay, float n) { return n == 0.0f ? 1.0f : expf(log_decay * n); }

@@ -55,7 +55,7 @@ constexpr int WALKERS = 148;                     // the plan, and with it the wo
 struct WalkArgs {
     alignas(64) CUtensorMap tm[3][3];            // q, k, v of each role: [B][T][H][width]
     MixArgs m;
-    int units, chunks;                           // (role, sequence, head), chunks of each
+    int nothing_comes, chunks;                   // test hook of the waits' limits; chunks of a (role, sequence, head)
     int walkers, rounds, rest;                   // blocks; units that each takes whole, and units left over, which are cut over all blocks
     int whole_steps;                             // rounds times chunks
     float *local, *starts;                       // [walkers][32][128][4] sums of stretches, and the states in front of them; null: no sequence is cut
@@ -205,7 +205,7 @@ template <int MODE> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kerne
         reg_dec<40>();   // once for all four warps: a warpgroup executes the same setmaxnreg together
         if (warp == COPY_WARP) {
             // ---- copies: k and v one chunk ahead of q
-            if (elect_one()) {
+            if (elect_one() && !p.nothing_comes) {
                 auto wait = [&](int bar, uint32_t parity) { ok = ok && mbar_wait_spin(BAR(bar), parity, spin, abort_flag); return ok; };
                 Step st = step_at(base + SM_STEPS), ahead = st;
                 auto load_kv = [&](int s) {
@@ -213,7 +213,7 @@ template <int MODE> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kerne
                     const int k = s & 1;
                     if (!wait(KVE + k, (s >> 1 & 1) ^ 1)) return;
                     load_tile(p, 1, ahead, r.dk, base + SM_K + k * TILE, BAR(KF + k));
-                    if (!(p.m.flags & RGLRU_FLAG_TEST_CARRY_NEVER_ARRIVES)) load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
+                    load_tile(p, 2, ahead, r.dv, base + SM_V + k * TILE, BAR(VF + k));
                     advance<MODE>(ahead, p, s + 1, base + SM_STEPS + 32);
                 };
                 if (steps > 0) load_kv(0);
@@ -728,10 +728,10 @@ size_t sm100_mix_bytes(int roles, int B, int T, int H) {
     return w.rest == 0 ? 0 : (size_t)w.walkers * 128 * 128 * 2 * sizeof(float);
 }
 
-cudaError_t sm100_mix(const MixArgs &a, void *scratch, cudaStream_t st) {
+cudaError_t sm100_mix(const MixArgs &a, uint32_t flags, void *scratch, cudaStream_t st) {
     WalkArgs p{};
     p.m = a;
-    p.units = a.roles * a.B * a.H;
+    p.nothing_comes = (flags & RGLRU_FLAG_TEST_CARRY_NEVER_ARRIVES) != 0;
     p.chunks = (a.T + CH - 1) / CH;
     const WalkPlan plan = walk_plan(a.roles, a.B, a.T, a.H);
     p.walkers = plan.walkers; p.rounds = plan.rounds; p.rest = plan.rest;
