@@ -4,6 +4,7 @@
 
 #include <cuda_bf16.h>
 
+#include "rglru_io.cuh"
 #include "rglru_linattn.cuh"
 #include "sm100_ptx.cuh"
 
@@ -16,14 +17,6 @@ constexpr int MAX_WIDTH = 256;
 constexpr int MAX_STEP_DK = 4096, MAX_STEP_DV = INT_MAX - 1023;   // of the token step: q and k in shared memory; a block's last column, behind the row's end, still is an int
 constexpr int C = 32, GEN_THREADS = 256;   // tokens a chunk
 
-template <typename IO> __device__ __forceinline__ float at(const void *p, long long i) {
-    if constexpr (sizeof(IO) == 4) return ((const float *)p)[i];
-    else return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
-}
-template <typename IO> __device__ __forceinline__ void put(void *p, long long i, float v) {
-    if constexpr (sizeof(IO) == 4) ((float *)p)[i] = v;
-    else ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
-}
 // ---- any type and width: fp32 on the CUDA cores.
 // A block walks chunks of 32 tokens of a (role, sequence, head) for 32 CB columns of v, its part of the state in shared memory.  A chunk is
 //     far = q S,   P = q k^T (decayed, masked; over q's place),   out = P v + decay far,   S <- d^n S + (decayed k)^T v

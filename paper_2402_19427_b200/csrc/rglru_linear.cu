@@ -20,14 +20,6 @@ struct GenericGemm {
     long long a_m, a_k, b_n, b_k, M, N, K;
     LinearEpilogue e;
 };
-template <typename IO> __device__ __forceinline__ float at(const void *p, long long i) {
-    if constexpr (sizeof(IO) == 4) return ((const float *)p)[i];
-    else return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
-}
-template <typename IO> __device__ __forceinline__ void put(void *p, long long i, float v) {
-    if constexpr (sizeof(IO) == 4) ((float *)p)[i] = v;
-    else ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
-}
 template <typename IO> __global__ void __launch_bounds__(256) generic_linear_kernel(GenericGemm g) {
     __shared__ __align__(16) float sa[GK][GT + 4], sb[GK][GT + 4];
     dependency_wait();

@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "rglru_internal.h"
+#include "rglru_io.cuh"
 #include "sm100_ptx.cuh"
 
 namespace rglru {

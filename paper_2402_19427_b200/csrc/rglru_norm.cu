@@ -10,6 +10,7 @@
 #include <cuda_bf16.h>
 
 #include "rglru_internal.h"
+#include "rglru_io.cuh"
 #include "sm100_ptx.cuh"
 
 namespace rglru {
@@ -379,14 +380,6 @@ __global__ void __launch_bounds__(1024) norm_columns_kernel(const float *part, i
 }
 
 // Rows that no block holds in registers (4096 x 16384 bf16 backward 520 us): a block reads its row three times (the second and third time mostly out of L2).
-template <typename IO> __device__ __forceinline__ float at(const void *p, long long i) {
-    if constexpr (sizeof(IO) == 4) return ((const float *)p)[i];
-    else return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
-}
-template <typename IO> __device__ __forceinline__ void put(void *p, long long i, float v) {
-    const float f[1] = {v};
-    store_vec<IO, 1>((IO *)p + i, f);
-}
 template <typename IO> __global__ void __launch_bounds__(512) norm_long_kernel(NormArgs a) {
     __shared__ __align__(16) float red[2][1][16];
     dependency_wait();

@@ -577,7 +577,7 @@ template <int MODE> __global__ void __launch_bounds__(THREADS, 1) mix_walk_kerne
                     if (e0 + j < r.dv) *(float4 *)(dst + j) = make_float4(S2[j / 2].x, S2[j / 2].y, S2[j / 2 + 1].x, S2[j / 2 + 1].y);
             }
         }
-if (STATE_ONLY && steps > 0 && ok) {
+        if (STATE_ONLY && steps > 0 && ok) {
             float4 *l = (float4 *)p.local + ((size_t)blockIdx.x * 32 + e0 / 4) * 128 + d;
 #pragma unroll
             for (int j = 0; j < 16; ++j) l[j * 128] = make_float4(S2[2 * j].x, S2[2 * j].y, S2[2 * j + 1].x, S2[2 * j + 1].y);

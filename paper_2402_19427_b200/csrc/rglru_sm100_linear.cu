@@ -51,22 +51,9 @@ struct GemmArgs {
     int b_never_comes;                    // test hook of the waits' limits
 };
 
-// bf16 A and B, fp32 accumulator
-__device__ __forceinline__ uint32_t instruction(int M, int N, int a_turned, int b_turned) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_turned << 15) | ((uint32_t)b_turned << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-
-template <typename IO> __device__ __forceinline__ float ld1(const void *p, long long i) {
-    if constexpr (sizeof(IO) == 4) return ((const float *)p)[i];
-    else return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
-}
-template <typename IO> __device__ __forceinline__ void st1(void *p, long long i, float v) {
-    if constexpr (sizeof(IO) == 4) ((float *)p)[i] = v;
-    else ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
-}
 template <typename IO> __device__ __forceinline__ void finish_one(const LinearEpilogue &e, long long o, float z) {
-    if (e.preact) st1<IO>(e.preact, o, z);
-    st1<IO>(e.y, o, activate<sizeof(IO) == 2>(z, e.activation) + (e.residual ? ld1<IO>(e.residual, o) : 0.0f));
+    if (e.preact) put<IO>(e.preact, o, z);
+    put<IO>(e.y, o, activate<sizeof(IO) == 2>(z, e.activation) + (e.residual ? at<IO>(e.residual, o) : 0.0f));
 }
 // 32 neighbouring results of row m, v, to their place: a thread has a row, and writes whole sectors of it
 template <typename IO> __device__ __forceinline__ void finish_row(const GemmArgs &p, long long m, int n0, float *v) {
@@ -238,7 +225,7 @@ template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm
         }
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
-            const uint32_t idesc = instruction(256, p.NT, p.a_turned, p.b_turned);
+            const uint32_t idesc = make_idesc(256, p.NT) | (uint32_t)p.a_turned << 15 | (uint32_t)p.b_turned << 16;
             // 16 of K an instruction: 32 bytes along a row, or 16 rows (descriptors count in units of 16 bytes)
             const uint64_t a0 = p.a_turned ? make_desc_sw128_mn(base, MN_BLOCK) : make_desc_sw128(base), a_step = p.a_turned ? 128 : 2;
             const uint64_t b0 = p.b_turned ? make_desc_sw128_mn(base + A_BYTES, MN_BLOCK) : make_desc_sw128(base + A_BYTES), b_step = p.b_turned ? 128 : 2;

@@ -78,12 +78,6 @@ __device__ __forceinline__ bool mbar_wait_spin(uint32_t bar, uint32_t parity, un
         }
     }
 }
-// whether the barrier's phase has ended, without waiting for it
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
 __device__ __forceinline__ bool warp_wait_spin(uint32_t bar, uint32_t parity, unsigned long long limit_ns, volatile int *abort_flag) {
     return __all_sync(0xffffffffu, mbar_wait_spin(bar, parity, limit_ns, abort_flag));
 }
@@ -252,10 +246,6 @@ __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *tm) { asm 
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *tm, int c0, int t, int b, uint32_t src_smem) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
                  ::"l"(tm), "r"(c0), "r"(t), "r"(b), "r"(src_smem) : "memory");
-}
-__device__ __forceinline__ void tma_store_4d(const CUtensorMap *tm, int c0, int c1, int c2, int c3, uint32_t src_smem) {
-    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];"
-                 ::"l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(src_smem) : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
