@@ -124,3 +124,70 @@ def test_waits_that_run_out_are_reported_and_the_next_call_is_clean(which):
     assert all(torch.equal(a, b) for a, b in zip(call(0), want))
     torch.cuda.synchronize()
     assert binding.query_status(ws) == binding.OK
+
+
+@pytest.mark.parametrize("io,T", [("bf16", 9000), ("f32", 1100)])
+def test_a_captured_prompt_of_a_cut_sequence_updates_its_state_in_place(io, T):
+    """The copy of s0 that such a call makes for its blocks is captured with it, and made again on every replay"""
+    from paper_2402_19427_b200 import binding
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q, k, v = (torch.randn(1, T, 2, 64, generator=g, device="cuda").to(DT[io]) for _ in range(3))
+    ld, s0 = torch.tensor([-0.001, -0.0001], device="cuda"), torch.randn(1, 2, 64, 64, generator=g, device="cuda")
+    o1, s1 = binding.linear_attention_prefill(q, k, v, ld, s0=s0)
+    o2, s2 = binding.linear_attention_prefill(q, k, v, ld, s0=s1)
+    s = s0.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, _ = binding.linear_attention_prefill(q, k, v, ld, s0=s, s_T=s)
+    for want_o, want_s in ((o1, s1), (o2, s2)):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want_o) and torch.equal(s, want_s)
+
+
+@pytest.mark.parametrize("dk,dv", [(8, 8), (8, 128), (128, 8), (72, 8), (16, 120)])
+def test_the_narrowest_heads_of_the_tensor_core_walk(dk, dv):
+    from paper_2402_19427_b200 import binding
+    from test_gpu_linear_attention import check_backward, check_forward, make
+    for B, T, H in ((1, 1, 3), (2, 200, 3)):
+        t = make(B, T, H, dk, dv, "bf16")
+        o, s_T = binding.linear_attention_prefill(t["q"], t["k"], t["v"], t["ld"], s0=t["s0"])
+        check_forward(t, o, s_T, dk ** -0.5)
+        check_backward(t, binding.linear_attention_backward(t["q"], t["k"], t["v"], t["ld"], t["do"], s0=t["s0"], ds_T=t["ds_T"], state_grads=True), dk ** -0.5)
+
+
+def test_two_host_threads_call_at_once():
+    """Each with its stream; attributes of kernels and plans of a device are set up by whoever comes first"""
+    import threading
+    from paper_2402_19427_b200 import binding
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, w = torch.randn(300, 264, generator=g, device="cuda").bfloat16(), torch.randn(520, 264, generator=g, device="cuda").bfloat16()
+    q = x.view(1, 300, 3, 88)
+    ld = torch.full((3,), -0.01, device="cuda")
+
+    def work():
+        y, pre = binding.linear(x, w, activation="gelu", keep_preact=True)
+        grads = binding.linear_backward(y, x, w, preact=pre, activation="gelu")
+        n, mean, rstd = binding.layer_norm(y, stats=True)
+        return [y, *grads.values(), n, binding.layer_norm_backward(y, n, rstd, mean=mean)["weight"], *binding.linear_attention_prefill(q, q, q, ld),
+                *binding.linear_attention_backward(q, q, q, ld, q, state_grads=True).values()]
+
+    want, got, errors = work(), [[], []], []
+    torch.cuda.synchronize()
+
+    def run(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got[i].append(work())
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:   # noqa: BLE001
+            errors.append(e)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    assert all(torch.equal(a, b) for runs in got for r in runs for a, b in zip(r, want))
