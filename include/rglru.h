@@ -348,7 +348,8 @@ int32_t rglru_linear_backward(const rglru_linear_shape_t *shape, const void *dy,
  * Linear attention with a decay for each head, a mixer with a state of constant size like the RG-LRU, S [dk,dv] per head:
  *     S_t = d S_{t-1} + k_t v_t^T,   o_t = scale q_t S_t,   d = exp(log_decay[h])
  * d is a constant of the layer; no gradient is formed for it.  log_decay is usually negative; 0 is plain linear attention, -inf
- * forgets everything but the token itself, above 0 the state grows.
+ * forgets everything but the token itself, above 0 the state grows (up to 0.69, twofold a token: bf16 calls take powers over 128 tokens, which leave fp32's
+ * range beyond).
  *   q, k          [B,T,H,dk] io        v, o   [B,T,H,dv] io; o must not overlap q, k or v
  *   log_decay     [H] fp32
  *   s0            [B,H,dk,dv] fp32, in, or NULL for a zero state

@@ -37,7 +37,11 @@ bool sm100_mix_supported(const MixArgs &a, int io);
 size_t sm100_mix_bytes(int roles, int B, int T, int H);
 cudaError_t sm100_mix(const MixArgs &a, uint32_t flags, void *scratch, cudaStream_t st);
 
-// decay^n; n = 0 is 1 whatever the decay (log_decay may be minus infinity)
-__device__ __forceinline__ float decay_power(float log_decay, float n) { return n == 0.0f ? 1.0f : expf(log_decay * n); }
+// decay^n; n = 0 is 1 whatever the decay (log_decay may be minus infinity).  Powers beyond fp32's range are held at its largest number: what has grown out
+// of the range still comes out infinite, but a state that is 0 stays 0 (inf * 0 is NaN).
+__device__ __forceinline__ float decay_power(float log_decay, float n) {
+    const float e = n == 0.0f ? 1.0f : expf(log_decay * n);
+    return e > 3.402823466e38f ? 3.402823466e38f : e;
+}
 
 }  // namespace rglru

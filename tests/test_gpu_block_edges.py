@@ -191,3 +191,25 @@ def test_two_host_threads_call_at_once():
         t.join()
     assert not errors, errors
     assert all(torch.equal(a, b) for runs in got for r in runs for a, b in zip(r, want))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,H", [(1, 300, 3), (1, 19300, 3), (60, 1400, 3)])
+def test_growing_states_and_tokens_of_zeros(B, T, H, io):
+    """Powers of a decay above one that leave fp32's range take nothing from a state that is 0: sequences that are zeros but for their last tokens (forward) or
+    their first (backward) give what those tokens give alone"""
+    from paper_2402_19427_b200 import binding
+    from test_gpu_linear_attention import check_backward, check_forward, make
+    n, w = 90, 64
+    ld = [0.01, 0.3, 0.6][:H]
+    part = make(B, n, H, w, w, io, state=False, decay=ld)
+    zero = torch.zeros(B, T - n, H, w, dtype=DT[io], device="cuda")
+    late = {x: torch.cat([zero, part[x]], 1) for x in "qkv"}
+    o, s_T = binding.linear_attention_prefill(*(late[x] for x in "qkv"), part["ld"])
+    assert (o[:, :T - n] == 0).all()
+    check_forward(part, o[:, T - n:], s_T, w ** -0.5)
+    early = {x: torch.cat([part[x], zero], 1) for x in ("q", "k", "v", "do")}
+    got = binding.linear_attention_backward(early["q"], early["k"], early["v"], part["ld"], early["do"], state_grads=True)
+    for x in "kv":
+        assert (got[x][:, n:] == 0).all(), x
+    check_backward(part, {x: got[x][:, :n] if x != "s0" else got[x] for x in got}, w ** -0.5)
