@@ -23,7 +23,8 @@ constexpr int C = 32, GEN_THREADS = 256;   // tokens a chunk
 // A warp has 32 columns: lane (rg, cg) owns four of them and every fourth row, so that an operand read by 16 bytes serves 16 products and
 // comes without bank conflicts.  Bound by the CUDA cores' instructions (dk = dv = 128: some 16 thousand issue slots of each scheduler a chunk, 15 us of an
 // SM's, 55 % of the slots taken), with two blocks an SM so that one's loads and barriers lie under the other's products: q, k, v, S take half
-// the SM's shared memory to the byte, the powers of the decay lie in the padding of k's rows.  8 x 2048 tokens of 20 heads take 1.5 ms.
+// the SM's shared memory to the byte, the powers of the decay lie in the padding of k's rows.  8 x 2048 tokens of 20 heads take 1.5 ms, heads of 256
+// columns (one block an SM) 4 x 2048 tokens of 16 heads 3.2.
 // Long sequences of few heads are cut into equal segments: a first launch leaves the sums of each (STATE_ONLY), and a segment's block starts
 // from the state before it, folded in order (65536 tokens of 16 heads 4.0 ms, in one piece 25 ms).
 struct GenericArgs {

@@ -145,7 +145,7 @@ template <typename IO> cudaError_t few_rows(const GenericGemm &g, cudaStream_t s
     return g.K % MOST == 0 ? few_rows<IO, MOST>(g, st) : few_rows<IO, 1>(g, st);
 }
 
-// dz = dy act'(z) in the io type, and the sums of the unrounded dz over a block's rows.  A thread owns VE columns and walks rows.  16384 x 2560 with
+// dz = dy act'(z) in the io type (the type of both products' operands; a second bf16 plane would double them), and the sums of the unrounded dz over a block's rows.  A thread owns VE columns and walks rows.  16384 x 2560 with
 // GeLU: 47 us for 252 MB, bound by the slope's instructions (72 % of the issue slots); the sums alone 19 us for 84 MB.
 struct DzArgs {
     long long M;

@@ -6,7 +6,7 @@
 // two buffers: the epilogue of one tile runs beside the products of the next.  Products of few tokens have the weights as A and the
 // tokens as B (a tile of 256 outputs and 32 to 128 tokens), and K split over the SMs: they are bound by reading the weights.
 //
-// 16384 x 2560 x 2560 in bf16 takes 143 us (1500 TFLOP/s, the tensor pipe 89 % busy), with GeLU and the pre-activation 159; dx 143, dW 158.  Narrow
+// 16384 x 2560 x 2560 in bf16 takes 143 us (1500 TFLOP/s, the tensor pipe 89 % busy), with GeLU and the pre-activation 159; dx 143, dW 148; dW of 131072 rows 1201.  Narrow
 // tiles are bound by their copies out of L2, 52 to 55 bytes a cycle and SM.
 //
 // fp32 operands are sums of three bf16 values; six of the nine products of those reach fp32's accuracy (what is left out is at
@@ -148,7 +148,7 @@ template <typename IO> __device__ __forceinline__ void finish_column(const GemmA
 
 // The tensor core cuts off what does not fit the sum so far, so an accumulator takes a limited number of terms.  fp32 io: it is emptied into registers every
 // DRAIN_BLOCKS K blocks (NT <= 128).  bf16: 16384 terms (some 2^-13 of the sum at worst, a sixteenth of the result's own half step), then its sum goes
-// on in fp32 in the block's place in `carry`, which a thread writes and reads back alone: 128 KB a CTA, out of L2, every 256 K blocks.
+// on in fp32 in the block's place in `carry`, which a thread writes and reads back alone: 128 KB a CTA, out of L2, every 256 K blocks (131072 rows of 2560 x 2560: 1430 TFLOP/s, 16384 rows 1450).
 constexpr int DRAIN_BLOCKS = 4, LONG_BLOCKS = 256;
 template <typename IO> __global__ void __launch_bounds__(THREADS, 1) linear_gemm_kernel(const __grid_constant__ GemmArgs p) {
     constexpr bool DRAIN = sizeof(IO) == 4;
