@@ -213,3 +213,21 @@ def test_growing_states_and_tokens_of_zeros(B, T, H, io):
     for x in "kv":
         assert (got[x][:, n:] == 0).all(), x
     check_backward(part, {x: got[x][:, :n] if x != "s0" else got[x] for x in got}, w ** -0.5)
+
+
+@pytest.mark.parametrize("kind", ["gelu", "silu"])
+def test_activations_to_bf16_are_good_to_their_last_place(kind):
+    """As far into the negative tail as bf16's normal numbers go: half a step of the result's own binade, and a tenth of that"""
+    from paper_2402_19427_b200 import binding
+    z = torch.cat([torch.linspace(-12.8, 12.8, 1 << 16, device="cuda"), torch.linspace(-1, 1, 1 << 12, device="cuda")]).bfloat16().unique()
+    one = torch.ones(1, 1, device="cuda", dtype=torch.bfloat16)
+    zd = z.double()
+    ref = zd * (0.5 * torch.special.erfc(-zd * 0.5 ** 0.5) if kind == "gelu" else torch.sigmoid(zd))
+    half = torch.exp2(torch.floor(torch.log2(ref.abs().clamp_min(2.0 ** -126))) - 8)
+    # Phi is good to 2e-7 and, relative to itself, to 1e-4; the exponential's and the reciprocal's arguments are rounded in fp32 (up to 122 half steps); both below 0.1
+    # of half a step, which is at least 2^-9 of the result
+    for rows in (z.numel(), 5):   # products on the tensor cores; few rows
+        x = z[:rows, None].contiguous() if rows > 5 else z[::max(1, z.numel() // 5)][:5, None].contiguous()
+        i = torch.arange(z.numel(), device="cuda") if rows > 5 else torch.arange(z.numel(), device="cuda")[::max(1, z.numel() // 5)][:5]
+        y = binding.linear(x, one, activation=kind)[:, 0]
+        bo.assert_within(kind, y, ref[i], 1.1 * half[i])
