@@ -231,3 +231,44 @@ def test_activations_to_bf16_are_good_to_their_last_place(kind):
         i = torch.arange(z.numel(), device="cuda") if rows > 5 else torch.arange(z.numel(), device="cuda")[::max(1, z.numel() // 5)][:5]
         y = binding.linear(x, one, activation=kind)[:, 0]
         bo.assert_within(kind, y, ref[i], 1.1 * half[i])
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_tensors_of_more_than_2_31_elements(io):
+    """The last rows and tokens of each operator are those of a call on them alone"""
+    from paper_2402_19427_b200 import binding
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rows, N, n = (1 << 31) // 1024 + 77, 1024, 5   # 2.1 10^9 elements and some
+    x = torch.empty(rows, N, device="cuda", dtype=DT[io])
+    x.fill_(0.25)
+    x[-200:] = torch.randn(200, N, generator=g, device="cuda").to(DT[io])
+    tail = x[-200:].clone()
+    y, mean, rstd = binding.layer_norm(x, stats=True)
+    assert torch.equal(y[-200:], binding.layer_norm(tail))
+    dx = binding.layer_norm_backward(y, x, rstd, mean=mean)["x"]
+    assert torch.equal(dx[-200:], binding.layer_norm_backward(y[-200:].clone(), tail, rstd[-200:].clone(), mean=mean[-200:].clone())["x"])
+    del y, dx
+    w = torch.randn(N, N, generator=g, device="cuda").to(DT[io])
+    y = binding.linear(x, w, residual=x)
+    ref, z, mag = bo.linear(tail, w, None, "none", tail)
+    bound = (2 * N + 4) * bo.U32 * mag + 16 * bo.U32 * (z.abs() + tail.double().abs()) + bo.half_step(DT[io]) * ref.abs()
+    bo.assert_within("y", y[-200:], ref, bound)
+    del y
+    got = binding.linear_backward(x, x, w, need=("x", "bias"))
+    dxr = tail.double() @ w.double()
+    bo.assert_within("dx", got["x"][-200:], dxr, 2 * N * bo.U32 * (tail.double().abs() @ w.double().abs()) + bo.half_step(DT[io]) * dxr.abs())
+    del got
+    # one sequence of 8 heads of 128: a decay that has forgotten all but the last 300 tokens (exp(-150) of what was before)
+    q = x.view(1, rows, 8, 128)
+    ld = torch.full((8,), -0.5, device="cuda")
+    o, s = binding.linear_attention_prefill(q, q, q, ld)
+    t = x[-300:].clone().view(1, 300, 8, 128)
+    orr, sr, om, sm = bo.attention(t, t, t, ld, None, 128 ** -0.5)
+    bo.assert_within("o", o[:, -n:], orr[:, -n:], bo.attention_bound(om[:, -n:], orr[:, -n:], DT[io], 300))
+    bo.assert_within("s_T", s, sr, bo.state_bound(sm, 300))
+    assert torch.isfinite(o[:, ::100003].float()).all()
+    del o
+    grads = binding.linear_attention_backward(q, q, q, ld, q)
+    ref, mag = bo.attention_backward(t, t, t, ld, t, None, None, 128 ** -0.5)
+    for name in "qkv":
+        bo.assert_within("d" + name, grads[name][:, -n:], ref[name][:, -n:], bo.attention_bound(mag[name][:, -n:], ref[name][:, -n:], DT[io], 300))
