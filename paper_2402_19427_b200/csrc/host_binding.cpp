@@ -247,6 +247,11 @@ int64_t integer(PyObject *o, const char *name) {
     if (v == -1 && PyErr_Occurred()) { PyErr_Clear(); TORCH_CHECK_TYPE(false, name, ": expected an integer"); }
     return v;
 }
+bool truth(PyObject *o, const char *name) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) { PyErr_Clear(); TORCH_CHECK_TYPE(false, name, ": expected True or False"); }
+    return v != 0;
+}
 int32_t int32_size(int64_t v, const char *name) {
     TORCH_CHECK_VALUE(v <= INT32_MAX, name, " is too large: ", v);
     return (int32_t)v;
@@ -293,7 +298,7 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     arguments(n, 7);
     const at::Tensor &x = required(a[0], "x");
     const at::Tensor *w = optional(a[1], "weight"), *b = optional(a[2], "bias"), *y = optional(a[6], "y");
-    const bool center = PyObject_IsTrue(a[4]) > 0, stats = PyObject_IsTrue(a[5]) > 0;
+    const bool center = truth(a[4], "center"), stats = truth(a[5], "stats");
     const rglru_norm_shape_t s = norm_shape(x, center, number(a[3], "eps"));
     const c10::Device dev = x.device();
     check(w, "weight", {s.N}, at::kFloat, dev); check(b, "bias", {s.N}, at::kFloat, dev); check(y, "y", x.sizes(), x.scalar_type(), dev);
@@ -326,7 +331,7 @@ PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
     arguments(n, 8);
     const at::Tensor &dy = required(a[0], "dy"), &x = required(a[1], "x"), &rstd = required(a[2], "rstd");
     const at::Tensor *mean = optional(a[3], "mean"), *w = optional(a[4], "weight"), *given = optional(a[6], "dx"), *ws = optional(a[7], "workspace");
-    const bool sums = PyObject_IsTrue(a[5]) > 0;
+    const bool sums = truth(a[5], "param_grads");
     const rglru_norm_shape_t s = norm_shape(x, mean != nullptr, 0.0);
     const c10::Device dev = x.device();
     const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
@@ -368,7 +373,7 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
     arguments(n, 9);
     const at::Tensor &x = required(a[0], "x"), &w = required(a[1], "weight");
     const at::Tensor *b = optional(a[2], "bias"), *res = optional(a[4], "residual"), *y = optional(a[5], "y"), *ws = optional(a[8], "workspace");
-    const bool keep = PyObject_IsTrue(a[6]) > 0;
+    const bool keep = truth(a[6], "keep_preact");
     TORCH_CHECK_VALUE(w.dim() == 2, "weight: expected [outputs, inputs], got ", w.sizes());
     const rglru_linear_shape_t s = linear_shape(x, "x", w.size(1), w, integer(a[3], "activation"), integer(a[7], "flags"));
     const c10::Device dev = w.device();
@@ -506,7 +511,7 @@ PyObject *linear_attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n
     const at::Tensor &q = required(a[0], "q"), &k = required(a[1], "k"), &v = required(a[2], "v"), &decay = required(a[3], "log_decay"), &dout = required(a[4], "do");
     const at::Tensor *s0 = optional(a[5], "s0"), *dsT = optional(a[6], "ds_T"), *gq = optional(a[9], "dq"), *gk = optional(a[10], "dk"), *gv = optional(a[11], "dv"),
                      *ws = optional(a[13], "workspace");
-    const bool want_state = PyObject_IsTrue(a[8]) > 0;
+    const bool want_state = truth(a[8], "state_grads");
     const rglru_linear_attention_shape_t s = mix_shape(q, v, 4, a[7], integer(a[12], "flags"));
     const c10::Device dev = q.device();
     const at::ScalarType io = q.scalar_type();

@@ -236,3 +236,19 @@ def test_outputs_over_vectors(b):
     for i in range(4):
         outs = [at(3) if i == j else at(7 + j) for j in range(4)]
         assert lib.rglru_linear_attention_backward(r(mix), None, at(0), at(1), at(2), at(3), at(4), at(5), at(6), *outs, at(11), 1 << 30, None) == b.ERR_ALIAS
+
+
+def test_truth_values_that_have_none(b):
+    """An argument whose truth cannot be told is named, instead of counting as False with an error left behind"""
+    x, q = torch.zeros(4, 64), torch.zeros(1, 4, 2, 16)
+    both = torch.tensor([True, False])
+    with pytest.raises(TypeError, match="center"):
+        b.layer_norm(x, center=both)
+    with pytest.raises(TypeError, match="stats"):
+        b.layer_norm(x, stats=both)
+    with pytest.raises(TypeError, match="param_grads"):
+        b.layer_norm_backward(x, x, x[:, 0], param_grads=both)
+    with pytest.raises(TypeError, match="keep_preact"):
+        b.linear(x, torch.zeros(8, 64), keep_preact=both)
+    with pytest.raises(TypeError, match="state_grads"):
+        b.linear_attention_backward(q, q, q, torch.zeros(2), q, state_grads=both)
